@@ -239,6 +239,119 @@ int deamoe_baseline_forward(const deamoe_config *cfg, int32_t T, const void *x,
 int deamoe_loaded_bytes(const deamoe_config *cfg, int32_t T, const int32_t *dept_count,
                         const int32_t *exp_count, int64_t *weight_bytes, int64_t *total_bytes);
 
+/* ---------------------------------------------------------------------------
+ * Operators beside the decode layer.  The conventions above hold, for batches
+ * of any size: tensors are row-major and contiguous, aligned to their element
+ * (stated where more is needed); outputs do not overlap inputs except where
+ * this header says so; T is at most DEAMOE_MAX_ROWS, widths at most
+ * DEAMOE_MAX_WIDTH.  Sums over no tokens are written as zeros. */
+#define DEAMOE_MAX_ROWS (1 << 23)
+#define DEAMOE_MAX_PAIRS (1 << 26)   /* T * k of the sorted tokens */
+
+/* --- Tokens sorted by expert and back (X^j and X^{j,i} of Sec. 3.2 as rows).
+ * A pair p = t * k + s is slot s of token t.  ids [T, k]: its group (expert or
+ * department), in any order, repeats allowed; an id outside [0, n) drops the
+ * pair (deamoe_route's topk_ids and its -1 padded tok_depts both fit).
+ *   offset [n + 1]   first row of every group; offset[n] = rows used
+ *   pair   [T * k]   pair of every row, by (group, pair) ascending; -1 from
+ *                    offset[n] on
+ *   row    [T, k]    row of every pair, -1 if dropped
+ * xs [T * k, h]: row r is x of token pair[r] / k; rows from offset[n] on are
+ * left as they were.  xs may be NULL (lists only; then x may be NULL too).
+ * n <= DEAMOE_MAX_EXPERTS, k <= DEAMOE_MAX_TOPK.  ws 16-byte aligned. */
+int deamoe_dispatch_workspace_bytes(int32_t T, int32_t k, int32_t n, size_t *bytes);
+int deamoe_dispatch(int32_t T, int32_t k, int32_t n, int32_t h, int32_t act_dtype,
+                    const int32_t *ids, const void *x, int32_t *offset, int32_t *pair,
+                    int32_t *row, void *xs, void *ws, size_t ws_bytes, void *stream);
+
+/* The gradient of x: dx[t] = sum over the token's pairs of dxs[row], in slot
+ * order, summed in fp32 and rounded once (zeros for a token without pairs). */
+int deamoe_dispatch_backward(int32_t T, int32_t k, int32_t h, int32_t act_dtype,
+                             const int32_t *row, const void *dxs, void *dx, void *stream);
+
+/* y[t] = sum over the token's pairs of w[t, s] * ys[row[t, s]], in slot order,
+ * summed in fp32 and rounded once (zeros for a token without pairs).  Weights
+ * of dropped pairs and rows that no pair has are not read. */
+int deamoe_combine(int32_t T, int32_t k, int32_t h, int32_t act_dtype, const int32_t *row,
+                   const float *w, const void *ys, void *y, void *stream);
+
+/* Its gradients: dys[row[t, s]] = w[t, s] * dy[t] (rows that no pair has are
+ * left as they were), dw[t, s] = <dy[t], ys[row[t, s]]> in fp32 (0 for a dropped
+ * pair).  dys or dw may be NULL; without dw, ys may be NULL, without dys, w. */
+int deamoe_combine_backward(int32_t T, int32_t k, int32_t h, int32_t act_dtype,
+                            const int32_t *row, const float *w, const void *ys, const void *dy,
+                            void *dys, float *dw, void *stream);
+
+/* --- Products with 4-bit weights and group scales.
+ * A weight is (q - 8) * scale: codes [n, R, K / 2], column 2j in the low and
+ * column 2j + 1 in the high four bits of byte j; scale [n, R, K / group], one
+ * for `group` consecutive columns of a row, fp32 or bf16.  x [M, K] and the
+ * outputs [M, R] are bf16; sums are fp32, a group's scale multiplies its whole
+ * sum, results are rounded once.
+ * offset (device, [n + 1], non-decreasing): rows offset[e] to offset[e + 1] of
+ * x meet matrix e (the lists of deamoe_dispatch); rows outside [offset[0],
+ * offset[n]) are left as they were; values outside [0, M] are taken as the
+ * nearer end.  NULL: one matrix (n == 1) for all rows.
+ * An infinity or NaN in a row of x makes that row of the output NaN.
+ * K a multiple of group; group 32, 64 or 128; any R; n <= DEAMOE_MAX_EXPERTS;
+ * codes and x 16-byte aligned. */
+typedef struct {
+  int32_t R;            /* rows of a matrix = columns of the output */
+  int32_t K;            /* columns of a matrix                      */
+  int32_t n;            /* matrices                                 */
+  int32_t group;        /* columns that share a scale               */
+  int32_t scale_dtype;  /* DEAMOE_F32 | DEAMOE_BF16                 */
+} deamoe_w4_config;
+
+/* y = x W^T */
+int deamoe_w4_linear(const deamoe_w4_config *cfg, int32_t M, const void *x, const int32_t *offset,
+                     const void *codes, const void *scale, void *y, void *stream);
+
+/* y = SiLU(x Wg^T) * (x Wu^T), both sums kept in fp32 */
+int deamoe_w4_swiglu(const deamoe_w4_config *cfg, int32_t M, const void *x, const int32_t *offset,
+                     const void *gate_codes, const void *gate_scale, const void *up_codes,
+                     const void *up_scale, void *y, void *stream);
+
+/* --- Norms around a block, with its gate and residual scale.
+ * RMSNorm: v^ = v * r, r = 1 / sqrt(mean(v^2) + eps), eps > 0.  All tensors
+ * are act_dtype, gradients of [h] parameters fp32.  Statistics, sums and
+ * everything between input and output are fp32; outputs are rounded once. */
+
+/* u = x^ * w, the input of a block.  u may be x. */
+int deamoe_prenorm(int32_t T, int32_t h, int32_t act_dtype, float eps, const void *x,
+                   const void *w, void *u, void *stream);
+
+/* dx = dres + the gradient of x from du (dres: the residual path's gradient,
+ * may be NULL, may be dx); dw [h] = sum over tokens of du * x^. */
+int deamoe_prenorm_backward(int32_t T, int32_t h, int32_t act_dtype, float eps, const void *x,
+                            const void *w, const void *du, const void *dres, void *dx, float *dw,
+                            void *ws, size_t ws_bytes, void *stream);
+
+/* z = res_scale * x + gate * (y^ * w): the block's output y joins the residual
+ * stream x.  gate: NULL (1), [h] for all tokens, or [T, h].
+ * u = z^ * w_next, the next block's input, of the rounded z (bit for bit what
+ * deamoe_prenorm makes of z); u and w_next are both NULL or both given.  z may
+ * be x. */
+#define DEAMOE_GATE_NONE 0
+#define DEAMOE_GATE_SHARED 1   /* [h]    */
+#define DEAMOE_GATE_FULL 2     /* [T, h] */
+int deamoe_postnorm(int32_t T, int32_t h, int32_t act_dtype, float eps, float res_scale,
+                    int32_t gate_mode, const void *x, const void *y, const void *w,
+                    const void *gate, const void *w_next, void *z, void *u, void *stream);
+
+/* Its gradients from dz and, with a next norm, du: with d = dz + the gradient
+ * of z from du, dx = res_scale * d (may be dz), dy through the norm, dw [h],
+ * dgate ([h] fp32 for a shared gate, [T, h] act_dtype for a full one),
+ * dw_next [h].  z, w_next, du, dw_next: all NULL or all given. */
+int deamoe_postnorm_backward(int32_t T, int32_t h, int32_t act_dtype, float eps, float res_scale,
+                             int32_t gate_mode, const void *y, const void *w, const void *gate,
+                             const void *z, const void *w_next, const void *dz, const void *du,
+                             void *dx, void *dy, float *dw, void *dgate, float *dw_next, void *ws,
+                             size_t ws_bytes, void *stream);
+
+/* Workspace of either gradient (16-byte aligned). */
+int deamoe_norm_workspace_bytes(int32_t T, int32_t h, size_t *bytes);
+
 #ifdef __cplusplus
 }
 #endif

@@ -1,0 +1,408 @@
+// RMSNorm before and after a block, with the block's gate and residual scale,
+// and their gradients.
+//
+//   v^ = v r,  r = 1 / sqrt(mean(v^2) + eps)
+//   u = x^ w                                          (before a block)
+//   z = a x + g (y^ w),  u = z^ w'                    (after it, and the next)
+// Gradients, with <m> the mean over a row:
+//   norm(v, q)  = r (q - v^ <q v^>)       q: gradient of v^
+//   d  = dz + norm(z, du w'),  dw' = sum_t du z^
+//   dx = a d,  dg = d y^ w,  dw = sum_t d g y^,  dy = norm(y, d g w)
+#include <type_traits>
+
+#include "ops.h"
+
+namespace deamoe {
+
+namespace {
+
+// Sums of N values over the workgroup, the same on every thread.  Two
+// reductions in a row use different halves of `s`, so that one barrier each is
+// enough.
+constexpr int kMaxWaves = 16, kMaxSums = 3;
+struct Reduce {
+  float (*s)[kMaxSums][kMaxWaves];
+  int flip = 0;
+  template <int N>
+  __device__ void sum(float (&v)[N]) {
+    const int waves = blockDim.x / kWave;
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+      for (int o = kWave / 2; o; o /= 2) v[i] += __shfl_xor(v[i], o);
+    if (waves == 1) return;
+    if (threadIdx.x % kWave == 0)
+#pragma unroll
+      for (int i = 0; i < N; ++i) s[flip][i][threadIdx.x / kWave] = v[i];
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      v[i] = 0.f;
+      for (int w = 0; w < waves; ++w) v[i] += s[flip][i][w];
+    }
+    flip ^= 1;
+  }
+};
+
+// The chunks of one row that a thread works on: chunk i starts at column
+// (i * threads + thread) * V.  N > 0: N chunks, held in registers; N == 0: rows
+// too wide for that are read again at every use.
+template <bool F32, int N>
+struct Row {
+  static constexpr int V = kVec<F32>;
+  const char *p;
+  int h;
+  Chunk<F32> held[N > 0 ? N : 1];
+  __device__ Row(const void *base, size_t t, int h_) : p(row_at<F32>(base, t, h_)), h(h_) {
+    if constexpr (N > 0)
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+        held[i] = load_chunk<F32>(p, (i * (int)blockDim.x + (int)threadIdx.x) * V, h);
+  }
+  __device__ Chunk<F32> get(int i, int c) const {
+    if constexpr (N > 0) return held[i];
+    return load_chunk<F32>(p, c, h);
+  }
+};
+
+// f(i, c) for every chunk of the thread; N > 0: also for those past the row's
+// end, whose loads give zeros and whose stores do nothing.
+template <bool F32, int N, class F>
+__device__ inline void chunks(int h, F f) {
+  constexpr int V = kVec<F32>;
+  if constexpr (N > 0) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) f(i, (i * (int)blockDim.x + (int)threadIdx.x) * V);
+  } else {
+    for (int c = threadIdx.x * V; c < h; c += blockDim.x * V) f(0, c);
+  }
+}
+
+__device__ inline float rms_factor(float sum, int h, float eps) {
+  return 1.0f / sqrtf(sum / (float)h + eps);
+}
+
+// u = x^ w of one row.
+template <bool F32, int N>
+__device__ inline void norm_row(const Row<F32, N> &x, const void *w, char *u, int h, float eps,
+                                Reduce &red) {
+  constexpr int V = kVec<F32>;
+  float ss[1] = {0.f};
+  chunks<F32, N>(h, [&](int i, int c) {
+    const Chunk<F32> v = x.get(i, c);
+#pragma unroll
+    for (int e = 0; e < V; ++e) ss[0] = __builtin_fmaf(v.at(e), v.at(e), ss[0]);
+  });
+  red.sum(ss);
+  const float r = rms_factor(ss[0], h, eps);
+  chunks<F32, N>(h, [&](int i, int c) {
+    const Chunk<F32> v = x.get(i, c), g = load_chunk<F32>(w, c, h);
+    float o[V];
+#pragma unroll
+    for (int e = 0; e < V; ++e) o[e] = v.at(e) * r * g.at(e);
+    store_chunk<F32>(u, c, h, pack_chunk<F32>(o));
+  });
+}
+
+}  // namespace
+
+template <bool F32, int N, int MAXG>
+__global__ __launch_bounds__(MAXG) void prenorm_kernel(PrenormArgs a) {
+  __shared__ float s_red[2][kMaxSums][kMaxWaves];
+  Reduce red{s_red};
+  for (int t = blockIdx.x; t < a.T; t += gridDim.x) {
+    const Row<F32, N> x(a.x, t, a.h);
+    norm_row<F32, N>(x, a.w, row_at<F32>(a.u, t, a.h), a.h, a.eps, red);
+  }
+}
+
+template <bool F32, int N, int MAXG>
+__global__ __launch_bounds__(MAXG) void postnorm_kernel(PostnormArgs a) {
+  constexpr int V = kVec<F32>;
+  __shared__ float s_red[2][kMaxSums][kMaxWaves];
+  Reduce red{s_red};
+  for (int t = blockIdx.x; t < a.T; t += gridDim.x) {
+    const Row<F32, N> y(a.y, t, a.h), x(a.x, t, a.h);
+    float ss[1] = {0.f};
+    chunks<F32, N>(a.h, [&](int i, int c) {
+      const Chunk<F32> v = y.get(i, c);
+#pragma unroll
+      for (int e = 0; e < V; ++e) ss[0] = __builtin_fmaf(v.at(e), v.at(e), ss[0]);
+    });
+    red.sum(ss);
+    const float r = rms_factor(ss[0], a.h, a.eps);
+    const char *gate = row_at<F32>(a.gate, a.gate_mode == DEAMOE_GATE_FULL ? t : 0, a.h);
+    char *zp = row_at<F32>(a.z, t, a.h);
+    Row<F32, N> z = x;
+    z.p = zp;
+    chunks<F32, N>(a.h, [&](int i, int c) {
+      const Chunk<F32> yv = y.get(i, c), xv = x.get(i, c), w = load_chunk<F32>(a.w, c, a.h);
+      float o[V];
+#pragma unroll
+      for (int e = 0; e < V; ++e) o[e] = yv.at(e) * r * w.at(e);
+      if (a.gate_mode != DEAMOE_GATE_NONE) {
+        const Chunk<F32> g = load_chunk<F32>(gate, c, a.h);
+#pragma unroll
+        for (int e = 0; e < V; ++e) o[e] *= g.at(e);
+      }
+#pragma unroll
+      for (int e = 0; e < V; ++e) o[e] = __builtin_fmaf(a.res_scale, xv.at(e), o[e]);
+      z.held[i] = pack_chunk<F32>(o);   // past the row's end: zeros, as loaded
+      store_chunk<F32>(zp, c, a.h, z.held[i]);
+    });
+    if (a.u) norm_row<F32, N>(z, a.w_next, row_at<F32>(a.u, t, a.h), a.h, a.eps, red);
+  }
+}
+
+// Gradients.  MODE: the norm before a block alone, the one after it alone, or
+// the one after it with the next one before.  A workgroup walks over rows t,
+// t + grid, ... and keeps its sums over them for its columns: in registers, or
+// for wide rows in its part of the workspace.
+enum NormMode : int { NORM_PRE = 0, NORM_POST = 1, NORM_BOTH = 2 };
+
+template <bool F32, int N, int MAXG, int MODE>
+__global__ __launch_bounds__(MAXG) void norm_backward_kernel(NormBackwardArgs a) {
+  constexpr int V = kVec<F32>, NH = N > 0 ? N : 1;
+  constexpr bool POST = MODE != NORM_PRE, NEXT = MODE != NORM_POST;
+  __shared__ float s_red[2][kMaxSums][kMaxWaves];
+  Reduce red{s_red};
+  const int h = a.h;
+  float *part = a.part + (size_t)blockIdx.x * 3 * h;   // dw, dw_next, dgate
+  float sum[3][NH][V] = {};
+  auto add = [&](int which, int i, int c, bool first, const float (&v)[V]) {
+    if constexpr (N > 0) {
+#pragma unroll
+      for (int e = 0; e < V; ++e) sum[which][i][e] += v[e];
+    } else {
+      for (int e = 0; e < V; ++e)
+        if (c + e < h) {
+          float *p = part + (size_t)which * h + c + e;
+          *p = first ? v[e] : *p + v[e];
+        }
+    }
+  };
+  for (int t = blockIdx.x; t < a.T; t += gridDim.x) {
+    const bool first = t == (int)blockIdx.x;
+    const Row<F32, NEXT ? N : 0> z(a.z, t, h), du(a.du, t, h);
+    const Row<F32, POST ? N : 0> y(a.y, t, h);
+    float s1[3] = {0.f, 0.f, 0.f};   // z^2, du w' z, y^2
+    chunks<F32, N>(h, [&](int i, int c) {
+      if constexpr (NEXT) {
+        const Chunk<F32> zv = z.get(i, c), g = du.get(i, c), w = load_chunk<F32>(a.w_next, c, h);
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          s1[0] = __builtin_fmaf(zv.at(e), zv.at(e), s1[0]);
+          s1[1] = __builtin_fmaf(g.at(e) * w.at(e), zv.at(e), s1[1]);
+        }
+      }
+      if constexpr (POST) {
+        const Chunk<F32> yv = y.get(i, c);
+#pragma unroll
+        for (int e = 0; e < V; ++e) s1[2] = __builtin_fmaf(yv.at(e), yv.at(e), s1[2]);
+      }
+    });
+    red.sum(s1);
+    const float rz = rms_factor(s1[0], h, a.eps), mz = s1[1] * rz / (float)h;
+    const float ry = rms_factor(s1[2], h, a.eps);
+    // d of one chunk: the gradient that reaches z
+    auto reach = [&](int i, int c, float (&d)[V]) {
+#pragma unroll
+      for (int e = 0; e < V; ++e) d[e] = 0.f;
+      if (a.dz) {
+        const Chunk<F32> v = load_chunk<F32>(row_at<F32>(a.dz, t, h), c, h);
+#pragma unroll
+        for (int e = 0; e < V; ++e) d[e] = v.at(e);
+      }
+      if constexpr (NEXT) {
+        const Chunk<F32> zv = z.get(i, c), g = du.get(i, c), w = load_chunk<F32>(a.w_next, c, h);
+#pragma unroll
+        for (int e = 0; e < V; ++e) d[e] += rz * (g.at(e) * w.at(e) - zv.at(e) * rz * mz);
+      }
+    };
+    const char *gate = row_at<F32>(a.gate, a.gate_mode == DEAMOE_GATE_FULL ? t : 0, h);
+    float dh[NH][V];   // d of every held chunk
+    float s2[1] = {0.f};
+    chunks<F32, N>(h, [&](int i, int c) {
+      reach(i, c, dh[i]);
+      if constexpr (POST) {
+        const Chunk<F32> yv = y.get(i, c), w = load_chunk<F32>(a.w, c, h);
+        float dn[V];
+#pragma unroll
+        for (int e = 0; e < V; ++e) dn[e] = dh[i][e];
+        if (a.gate_mode != DEAMOE_GATE_NONE) {
+          const Chunk<F32> g = load_chunk<F32>(gate, c, h);
+#pragma unroll
+          for (int e = 0; e < V; ++e) dn[e] *= g.at(e);
+        }
+#pragma unroll
+        for (int e = 0; e < V; ++e) s2[0] = __builtin_fmaf(dn[e] * w.at(e), yv.at(e) * ry, s2[0]);
+      }
+    });
+    if constexpr (POST) red.sum(s2);
+    const float my = s2[0] / (float)h;
+    chunks<F32, N>(h, [&](int i, int c) {
+      float d[V], o[V], g[V];
+      if constexpr (N > 0) {
+#pragma unroll
+        for (int e = 0; e < V; ++e) d[e] = dh[i][e];
+      } else {
+        reach(i, c, d);
+      }
+      if constexpr (NEXT) {
+        const Chunk<F32> zv = z.get(i, c), gv = du.get(i, c);
+#pragma unroll
+        for (int e = 0; e < V; ++e) o[e] = gv.at(e) * (zv.at(e) * rz);
+        add(1, i, c, first, o);
+      }
+      if constexpr (POST) {
+        const Chunk<F32> yv = y.get(i, c), w = load_chunk<F32>(a.w, c, h);
+        float dn[V];
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          dn[e] = d[e];
+          g[e] = d[e] * (yv.at(e) * ry * w.at(e));
+        }
+        if (a.gate_mode != DEAMOE_GATE_NONE) {
+          const Chunk<F32> gv = load_chunk<F32>(gate, c, h);
+#pragma unroll
+          for (int e = 0; e < V; ++e) dn[e] *= gv.at(e);
+          if (a.gate_mode == DEAMOE_GATE_FULL)
+            store_chunk<F32>(row_at<F32>(a.dgate, t, h), c, h, pack_chunk<F32>(g));
+          else
+            add(2, i, c, first, g);
+        }
+#pragma unroll
+        for (int e = 0; e < V; ++e) o[e] = dn[e] * (yv.at(e) * ry);
+        add(0, i, c, first, o);
+#pragma unroll
+        for (int e = 0; e < V; ++e) o[e] = ry * (dn[e] * w.at(e) - yv.at(e) * ry * my);
+        store_chunk<F32>(row_at<F32>(a.dy, t, h), c, h, pack_chunk<F32>(o));
+      }
+#pragma unroll
+      for (int e = 0; e < V; ++e) d[e] *= a.res_scale;
+      store_chunk<F32>(row_at<F32>(a.dx, t, h), c, h, pack_chunk<F32>(d));
+    });
+  }
+  if constexpr (N > 0)
+    chunks<F32, N>(h, [&](int i, int c) {
+#pragma unroll
+      for (int which = 0; which < 3; ++which) {
+        if ((which == 0 && !POST) || (which == 1 && !NEXT) ||
+            (which == 2 && (!POST || a.gate_mode != DEAMOE_GATE_SHARED)))
+          continue;
+#pragma unroll
+        for (int e = 0; e < V; ++e)
+          if (c + e < h) part[(size_t)which * h + c + e] = sum[which][i][e];
+      }
+    });
+}
+
+// out[which][c] = sum over the workgroups' parts, four interleaved sums joined.
+struct ColumnSumArgs {
+  const float *part;
+  float *out[3];
+  int32_t h, blocks;
+};
+__global__ __launch_bounds__(256) void column_sum_kernel(ColumnSumArgs a) {
+  __shared__ float s_sum[4][kWave];
+  const int which = blockIdx.y;
+  if (!a.out[which]) return;
+  const int lane = threadIdx.x % kWave, wv = threadIdx.x / kWave;
+  const int c = blockIdx.x * kWave + lane;
+  float v = 0.f;
+  if (c < a.h)
+    for (int b = wv; b < a.blocks; b += 4) v += a.part[((size_t)b * 3 + which) * a.h + c];
+  s_sum[wv][lane] = v;
+  __syncthreads();
+  if (wv == 0 && c < a.h)
+    a.out[which][c] = (s_sum[0][lane] + s_sum[1][lane]) + (s_sum[2][lane] + s_sum[3][lane]);
+}
+
+namespace {
+
+// Threads and held chunks per thread for a row: up to two chunks of 16 bytes
+// each and 1024 threads; wider rows are not held.
+struct Shape {
+  int threads, held;
+};
+Shape shape_of(int h, int act_f32) {
+  const int chunks = (h + (act_f32 ? 3 : 7)) / (act_f32 ? 4 : 8);
+  if (chunks <= 64) return {64, 1};
+  if (chunks <= 128) return {128, 1};
+  if (chunks <= 256) return {256, 1};
+  if (chunks <= 512) return {256, 2};
+  if (chunks <= 1024) return {512, 2};
+  if (chunks <= 2048) return {1024, 2};
+  return {1024, 0};
+}
+constexpr int kRowGrid = 1 << 16;   // workgroups at most; further rows are walked to
+
+template <bool F32, int N, int MAXG>
+hipError_t backward_shaped(const NormBackwardArgs &a, int threads, int blocks, hipStream_t s) {
+  if (!a.y)
+    hipLaunchKernelGGL((norm_backward_kernel<F32, N, MAXG, NORM_PRE>), dim3(blocks), dim3(threads),
+                       0, s, a);
+  else if (a.du)
+    hipLaunchKernelGGL((norm_backward_kernel<F32, N, MAXG, NORM_BOTH>), dim3(blocks),
+                       dim3(threads), 0, s, a);
+  else
+    hipLaunchKernelGGL((norm_backward_kernel<F32, N, MAXG, NORM_POST>), dim3(blocks),
+                       dim3(threads), 0, s, a);
+  return hipGetLastError();
+}
+
+// f(type, held, threads at most) with the row's shape as constants
+template <class F>
+hipError_t with_shape(Shape sh, bool f32, F f) {
+  using std::integral_constant;
+  auto typed = [&](auto F32) {
+    if (sh.held == 0) return f(F32, integral_constant<int, 0>{}, integral_constant<int, 1024>{});
+    if (sh.threads == 1024)
+      return f(F32, integral_constant<int, 2>{}, integral_constant<int, 1024>{});
+    if (sh.held == 2) return f(F32, integral_constant<int, 2>{}, integral_constant<int, 512>{});
+    return f(F32, integral_constant<int, 1>{}, integral_constant<int, 256>{});
+  };
+  return f32 ? typed(integral_constant<bool, true>{}) : typed(integral_constant<bool, false>{});
+}
+
+}  // namespace
+
+int norm_backward_blocks(int T, int) { return T < 512 ? T : 512; }
+
+hipError_t launch_prenorm(const PrenormArgs &a, hipStream_t s) {
+  const Shape sh = shape_of(a.h, a.act_f32);
+  return with_shape(sh, a.act_f32, [&](auto F32, auto N, auto G) {
+    hipLaunchKernelGGL((prenorm_kernel<F32.value, N.value, G.value>),
+                       dim3(a.T < kRowGrid ? a.T : kRowGrid), dim3(sh.threads), 0, s, a);
+    return hipGetLastError();
+  });
+}
+
+hipError_t launch_postnorm(const PostnormArgs &a, hipStream_t s) {
+  const Shape sh = shape_of(a.h, a.act_f32);
+  return with_shape(sh, a.act_f32, [&](auto F32, auto N, auto G) {
+    hipLaunchKernelGGL((postnorm_kernel<F32.value, N.value, G.value>),
+                       dim3(a.T < kRowGrid ? a.T : kRowGrid), dim3(sh.threads), 0, s, a);
+    return hipGetLastError();
+  });
+}
+
+hipError_t launch_norm_backward(const NormBackwardArgs &a, hipStream_t s) {
+  const Shape sh = shape_of(a.h, a.act_f32);
+  const int blocks = norm_backward_blocks(a.T, a.h);
+  const hipError_t e = with_shape(sh, a.act_f32, [&](auto F32, auto N, auto G) {
+    return backward_shaped<F32.value, N.value, G.value>(a, sh.threads, blocks, s);
+  });
+  if (e != hipSuccess) return e;
+  ColumnSumArgs c;
+  c.part = a.part;
+  c.out[0] = a.y ? a.dw : nullptr;
+  c.out[1] = a.dw_next;
+  c.out[2] = a.gate_mode == DEAMOE_GATE_SHARED ? static_cast<float *>(a.dgate) : nullptr;
+  c.h = a.h;
+  c.blocks = blocks;
+  hipLaunchKernelGGL(column_sum_kernel, dim3((a.h + kWave - 1) / kWave, 3), dim3(256), 0, s, c);
+  return hipGetLastError();
+}
+
+}  // namespace deamoe

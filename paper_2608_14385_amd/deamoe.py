@@ -26,7 +26,11 @@ SCRATCH_BYTES = 64 << 20   # library-owned workspace of deamoe_layer_forward_noa
 
 EXPORTS = ("deamoe_status_string", "deamoe_workspace_bytes", "deamoe_route",
            "deamoe_layer_forward", "deamoe_layer_forward_traced", "deamoe_baseline_forward",
-           "deamoe_loaded_bytes", "deamoe_trace_points", "deamoe_layer_forward_noalloc")
+           "deamoe_loaded_bytes", "deamoe_trace_points", "deamoe_layer_forward_noalloc",
+           "deamoe_dispatch_workspace_bytes", "deamoe_dispatch", "deamoe_dispatch_backward",
+           "deamoe_combine", "deamoe_combine_backward", "deamoe_w4_linear", "deamoe_w4_swiglu",
+           "deamoe_prenorm", "deamoe_prenorm_backward", "deamoe_postnorm",
+           "deamoe_postnorm_backward", "deamoe_norm_workspace_bytes")
 
 
 class DeamoeError(RuntimeError):
@@ -57,6 +61,12 @@ class deamoe_routing(C.Structure):
     _fields_ = [(f, C.c_void_p) for f in ROUTING_FIELDS]
 
 
+class deamoe_w4_config(C.Structure):
+    _fields_ = [(f, C.c_int32) for f in ("R", "K", "n", "group", "scale_dtype")]
+
+
+GATE_NONE, GATE_SHARED, GATE_FULL = 0, 1, 2
+
 _lib = None
 
 
@@ -84,6 +94,19 @@ def lib():
         L.deamoe_trace_points.argtypes = [cfgp, i32, C.POINTER(C.c_int32)]
         L.deamoe_loaded_bytes.argtypes = [cfgp, i32, vp, vp, C.POINTER(C.c_int64),
                                           C.POINTER(C.c_int64)]
+        sz, f32, szp, w4p = C.c_size_t, C.c_float, C.POINTER(C.c_size_t), C.POINTER(deamoe_w4_config)
+        L.deamoe_dispatch_workspace_bytes.argtypes = [i32, i32, i32, szp]
+        L.deamoe_dispatch.argtypes = [i32] * 5 + [vp] * 7 + [sz, vp]
+        L.deamoe_dispatch_backward.argtypes = [i32] * 4 + [vp] * 4
+        L.deamoe_combine.argtypes = [i32] * 4 + [vp] * 5
+        L.deamoe_combine_backward.argtypes = [i32] * 4 + [vp] * 7
+        L.deamoe_w4_linear.argtypes = [w4p, i32] + [vp] * 6
+        L.deamoe_w4_swiglu.argtypes = [w4p, i32] + [vp] * 8
+        L.deamoe_prenorm.argtypes = [i32] * 3 + [f32] + [vp] * 4
+        L.deamoe_prenorm_backward.argtypes = [i32] * 3 + [f32] + [vp] * 7 + [sz, vp]
+        L.deamoe_postnorm.argtypes = [i32] * 3 + [f32, f32, i32] + [vp] * 8
+        L.deamoe_postnorm_backward.argtypes = [i32] * 3 + [f32, f32, i32] + [vp] * 13 + [sz, vp]
+        L.deamoe_norm_workspace_bytes.argtypes = [i32, i32, szp]
         for f in EXPORTS:
             getattr(L, f).restype = C.c_int if f != "deamoe_status_string" else C.c_char_p
         _lib = L
@@ -258,3 +281,283 @@ class Layer:
         fn(self.c, x, self.W, y, self.ws, logits_in=logits_in, router_bias=router_bias,
            routing=routing, stream=stream)
         return y
+
+
+# ---------------------------------------------------------------------------
+# Operators beside the layer: sorted tokens, 4-bit products, norms.  Tensors
+# are contiguous and on one device, outputs are the caller's; the calls run on
+# `stream` (default: the current stream of the tensors' device) and, where no
+# workspace is given, take one from torch's allocator for that stream.
+
+
+def _fits(what: str, dev, **tensors):
+    """Every (tensor, dtype, shape) has that type and shape, is contiguous and on `dev`."""
+    for name, (t, dtype, shape) in tensors.items():
+        if t.dtype is not dtype or t.shape != shape:
+            raise DeamoeError(ERR_INVALID, f"{what}: {name} is {t.dtype} {tuple(t.shape)}, "
+                                           f"needed is {dtype} {tuple(shape)}")
+        if not t.is_contiguous() or t.device != dev:
+            raise DeamoeError(ERR_INVALID, f"{what}: {name} is not contiguous, or not on {dev}")
+
+
+def _act(what: str, t: torch.Tensor) -> int:
+    if t.dtype is torch.bfloat16:
+        return BF16
+    if t.dtype is torch.float32:
+        return F32
+    raise DeamoeError(ERR_INVALID, f"{what}: {t.dtype} is neither bfloat16 nor float32")
+
+
+def _run(fn, dev, stream, *args):
+    """fn(*args, stream) with the tensors' device current."""
+    if dev.type != "cuda":
+        raise DeamoeError(ERR_INVALID, f"{fn.__name__}: tensors are on {dev}, not on a GPU")
+    if dev.index == torch.cuda.current_device():
+        status = fn(*args, _stream(stream))
+    else:
+        with torch.cuda.device(dev):
+            status = fn(*args, _stream(stream))
+    _check(status, fn.__name__)
+
+
+def _workspace(ws, dev, stream, nbytes: int):
+    """(pointer, size) and the tensor that keeps it: `ws`, or one of torch's for `stream`."""
+    if ws is None and nbytes and dev.type == "cuda":
+        if stream is None:
+            ws = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+        else:
+            with torch.cuda.stream(stream):
+                ws = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+    elif ws is not None and (ws.device != dev or not ws.is_contiguous()):
+        raise DeamoeError(ERR_WORKSPACE, f"workspace is not contiguous, or not on {dev}")
+    return (None, 0, None) if ws is None else (ws.data_ptr(), ws.numel() * ws.element_size(), ws)
+
+
+def _bytes(fn, *args) -> int:
+    n = C.c_size_t(0)
+    _check(fn(*args, C.byref(n)), fn.__name__)
+    return n.value
+
+
+def _rows(what: str, t: torch.Tensor, name: str) -> tuple:
+    if t.dim() != 2:
+        raise DeamoeError(ERR_INVALID, f"{what}: {name} has {t.dim()} dimensions, needed are 2")
+    return t.shape
+
+
+def deamoe_dispatch_workspace_bytes(T: int, k: int, n: int) -> int:
+    return _bytes(lib().deamoe_dispatch_workspace_bytes, T, k, n)
+
+
+def deamoe_dispatch(ids, x, offset, pair, row, xs=None, ws=None, stream=None):
+    """Tokens sorted by group: ids [T, k] int32 -> offset [n + 1], pair [T * k], row [T, k], and
+    with xs [T * k, h] the rows of x [T, h] in that order (x may be None without xs)."""
+    what, i32 = "deamoe_dispatch", torch.int32
+    T, k = _rows(what, ids, "ids")
+    dev, n, h, act = ids.device, offset.numel() - 1, 1, F32
+    _fits(what, dev, ids=(ids, i32, ids.shape), offset=(offset, i32, (n + 1,)),
+          pair=(pair, i32, (T * k,)), row=(row, i32, (T, k)))
+    if xs is not None:
+        act, h = _act(what, x), _rows(what, x, "x")[1]
+        _fits(what, dev, x=(x, x.dtype, (T, h)), xs=(xs, x.dtype, (T * k, h)))
+    wp, wn, keep = _workspace(ws, dev, stream, deamoe_dispatch_workspace_bytes(T, k, n))
+    _run(lib().deamoe_dispatch, dev, stream, T, k, n, h, act, ids.data_ptr(),
+         _ptr(x) if xs is not None else None, offset.data_ptr(), pair.data_ptr(), row.data_ptr(),
+         _ptr(xs), wp, wn)
+
+
+def deamoe_dispatch_backward(row, dxs, dx, stream=None):
+    """dx [T, h]: the sum of each token's rows of dxs [T * k, h]."""
+    what = "deamoe_dispatch_backward"
+    (T, k), h, dev = _rows(what, row, "row"), _rows(what, dx, "dx")[1], row.device
+    act = _act(what, dx)
+    _fits(what, dev, row=(row, torch.int32, (T, k)), dx=(dx, dx.dtype, (T, h)),
+          dxs=(dxs, dx.dtype, (T * k, h)))
+    _run(lib().deamoe_dispatch_backward, dev, stream, T, k, h, act, row.data_ptr(),
+         dxs.data_ptr(), dx.data_ptr())
+
+
+def deamoe_combine(row, w, ys, y, stream=None):
+    """y [T, h]: the sum of each token's rows of ys [T * k, h], weighted by w [T, k] (fp32)."""
+    what = "deamoe_combine"
+    (T, k), h, dev = _rows(what, row, "row"), _rows(what, y, "y")[1], row.device
+    act = _act(what, y)
+    _fits(what, dev, row=(row, torch.int32, (T, k)), w=(w, torch.float32, (T, k)),
+          y=(y, y.dtype, (T, h)), ys=(ys, y.dtype, (T * k, h)))
+    _run(lib().deamoe_combine, dev, stream, T, k, h, act, row.data_ptr(), w.data_ptr(),
+         ys.data_ptr(), y.data_ptr())
+
+
+def deamoe_combine_backward(row, w, ys, dy, dys=None, dw=None, stream=None):
+    """dys [T * k, h] and dw [T, k] (either may be None) from dy [T, h]; w is needed for dys only,
+    ys for dw only."""
+    what = "deamoe_combine_backward"
+    (T, k), h, dev = _rows(what, row, "row"), _rows(what, dy, "dy")[1], row.device
+    act, f32 = _act(what, dy), torch.float32
+    _fits(what, dev, row=(row, torch.int32, (T, k)), dy=(dy, dy.dtype, (T, h)),
+          **({"dys": (dys, dy.dtype, (T * k, h)), "w": (w, f32, (T, k))} if dys is not None else {}),
+          **({"dw": (dw, f32, (T, k)), "ys": (ys, dy.dtype, (T * k, h))} if dw is not None else {}))
+    _run(lib().deamoe_combine_backward, dev, stream, T, k, h, act, row.data_ptr(),
+         _ptr(w) if dys is not None else None, _ptr(ys) if dw is not None else None, dy.data_ptr(),
+         _ptr(dys), _ptr(dw))
+
+
+def _w4(what: str, x, matrices, y, offset):
+    """Checks one product's tensors: its config, rows and device."""
+    codes, scale = matrices[0]
+    M, K = _rows(what, x, "x")
+    R, half = codes.shape[-2:] if codes.dim() > 1 else (0, 0)
+    if codes.dim() not in (2, 3) or half * 2 != K or scale.dim() != codes.dim() or not scale.shape[-1]:
+        raise DeamoeError(ERR_INVALID, f"{what}: codes {tuple(codes.shape)} and scale "
+                                       f"{tuple(scale.shape)} do not fit {K} columns")
+    n = codes.shape[0] if codes.dim() == 3 else 1
+    group, dev, sdt = K // scale.shape[-1], x.device, scale.dtype
+    if group * scale.shape[-1] != K or sdt not in (torch.float32, torch.bfloat16):
+        raise DeamoeError(ERR_INVALID, f"{what}: scale is {sdt} {tuple(scale.shape)} for {K} columns")
+    for c, s in matrices:
+        _fits(what, dev, codes=(c, torch.uint8, codes.shape),
+              scale=(s, sdt, (*codes.shape[:-1], K // group)))
+    _fits(what, dev, x=(x, torch.bfloat16, (M, K)), y=(y, torch.bfloat16, (M, R)))
+    if offset is not None:
+        _fits(what, dev, offset=(offset, torch.int32, (n + 1,)))
+    cfg = deamoe_w4_config(R=R, K=K, n=n, group=group,
+                           scale_dtype=BF16 if sdt is torch.bfloat16 else F32)
+    return cfg, M, dev
+
+
+def deamoe_w4_linear(x, codes, scale, y, offset=None, stream=None):
+    """y [M, R] = x [M, K] W^T (bf16); codes [R, K / 2] uint8 and scale [R, K / group], or stacks of
+    n of both with offset [n + 1] (int32): the rows of every matrix."""
+    cfg, M, dev = _w4("deamoe_w4_linear", x, ((codes, scale),), y, offset)
+    _run(lib().deamoe_w4_linear, dev, stream, C.byref(cfg), M, x.data_ptr(), _ptr(offset),
+         codes.data_ptr(), scale.data_ptr(), y.data_ptr())
+
+
+def deamoe_w4_swiglu(x, gate_codes, gate_scale, up_codes, up_scale, y, offset=None, stream=None):
+    """y = SiLU(x Wg^T) * (x Wu^T), otherwise as deamoe_w4_linear."""
+    cfg, M, dev = _w4("deamoe_w4_swiglu", x, ((gate_codes, gate_scale), (up_codes, up_scale)), y,
+                      offset)
+    _run(lib().deamoe_w4_swiglu, dev, stream, C.byref(cfg), M, x.data_ptr(), _ptr(offset),
+         gate_codes.data_ptr(), gate_scale.data_ptr(), up_codes.data_ptr(), up_scale.data_ptr(),
+         y.data_ptr())
+
+
+def deamoe_norm_workspace_bytes(T: int, h: int) -> int:
+    return _bytes(lib().deamoe_norm_workspace_bytes, T, h)
+
+
+def deamoe_prenorm(x, w, u, eps: float = 1e-6, stream=None):
+    """u = RMSNorm(x) * w, rows of x [T, h]; u may be x."""
+    what = "deamoe_prenorm"
+    (T, h), act, dev, dt = _rows(what, x, "x"), _act(what, x), x.device, x.dtype
+    _fits(what, dev, x=(x, dt, (T, h)), w=(w, dt, (h,)), u=(u, dt, (T, h)))
+    _run(lib().deamoe_prenorm, dev, stream, T, h, act, eps, x.data_ptr(), w.data_ptr(),
+         u.data_ptr())
+
+
+def deamoe_prenorm_backward(x, w, du, dx, dw, dres=None, eps: float = 1e-6, ws=None, stream=None):
+    """dx = dres + the gradient of x from du; dw [h] fp32.  dres may be dx."""
+    what, f32 = "deamoe_prenorm_backward", torch.float32
+    (T, h), act, dev, dt = _rows(what, x, "x"), _act(what, x), x.device, x.dtype
+    _fits(what, dev, x=(x, dt, (T, h)), w=(w, dt, (h,)), du=(du, dt, (T, h)), dx=(dx, dt, (T, h)),
+          dw=(dw, f32, (h,)), **({"dres": (dres, dt, (T, h))} if dres is not None else {}))
+    wp, wn, keep = _workspace(ws, dev, stream, deamoe_norm_workspace_bytes(T, h))
+    _run(lib().deamoe_prenorm_backward, dev, stream, T, h, act, eps, x.data_ptr(), w.data_ptr(),
+         du.data_ptr(), _ptr(dres), dx.data_ptr(), dw.data_ptr(), wp, wn)
+
+
+def _gate(what, gate, T, h, dt, dev) -> int:
+    if gate is None:
+        return GATE_NONE
+    _fits(what, dev, gate=(gate, dt, (h,) if gate.dim() == 1 else (T, h)))
+    return GATE_SHARED if gate.dim() == 1 else GATE_FULL
+
+
+def deamoe_postnorm(x, y, w, z, gate=None, res_scale: float = 1.0, w_next=None, u=None,
+                    eps: float = 1e-6, stream=None):
+    """z = res_scale * x + gate * RMSNorm(y) * w, rows of x and y [T, h]; gate [h], [T, h] or None (1).
+    With w_next and u also u = RMSNorm(z) * w_next.  z may be x."""
+    what = "deamoe_postnorm"
+    (T, h), act, dev, dt = _rows(what, x, "x"), _act(what, x), x.device, x.dtype
+    _fits(what, dev, x=(x, dt, (T, h)), y=(y, dt, (T, h)), w=(w, dt, (h,)), z=(z, dt, (T, h)),
+          **({"w_next": (w_next, dt, (h,))} if w_next is not None else {}),
+          **({"u": (u, dt, (T, h))} if u is not None else {}))
+    mode = _gate(what, gate, T, h, dt, dev)
+    _run(lib().deamoe_postnorm, dev, stream, T, h, act, eps, res_scale, mode, x.data_ptr(),
+         y.data_ptr(), w.data_ptr(), _ptr(gate), _ptr(w_next), z.data_ptr(), _ptr(u))
+
+
+def deamoe_postnorm_backward(y, w, dz, dx, dy, dw, gate=None, dgate=None, res_scale: float = 1.0,
+                             z=None, w_next=None, du=None, dw_next=None, eps: float = 1e-6, ws=None,
+                             stream=None):
+    """Gradients of deamoe_postnorm from dz and, with a next norm (z, w_next, du, dw_next), du: dx, dy
+    [T, h], dw and dw_next [h] fp32, dgate as the gate ([h]: fp32).  dx may be dz."""
+    what, f32 = "deamoe_postnorm_backward", torch.float32
+    (T, h), act, dev, dt = _rows(what, y, "y"), _act(what, y), y.device, y.dtype
+    mode, full, vec = _gate(what, gate, T, h, dt, dev), (T, h), (h,)
+    _fits(what, dev, y=(y, dt, full), w=(w, dt, vec), dz=(dz, dt, full), dx=(dx, dt, full),
+          dy=(dy, dt, full), dw=(dw, f32, vec))
+    if (dgate is None) != (mode == GATE_NONE) or len({t is None for t in (z, w_next, du, dw_next)}) != 1:
+        raise DeamoeError(ERR_INVALID, f"{what}: gate and dgate, and z, w_next, du and dw_next, are "
+                                       "given together or not at all")
+    if dgate is not None:
+        _fits(what, dev, dgate=(dgate, f32, vec) if mode == GATE_SHARED else (dgate, dt, full))
+    if du is not None:
+        _fits(what, dev, z=(z, dt, full), w_next=(w_next, dt, vec), du=(du, dt, full),
+              dw_next=(dw_next, f32, vec))
+    wp, wn, keep = _workspace(ws, dev, stream, deamoe_norm_workspace_bytes(T, h))
+    _run(lib().deamoe_postnorm_backward, dev, stream, T, h, act, eps, res_scale, mode, y.data_ptr(),
+         w.data_ptr(), _ptr(gate), _ptr(z), _ptr(w_next), dz.data_ptr(), _ptr(du), dx.data_ptr(),
+         dy.data_ptr(), dw.data_ptr(), _ptr(dgate), _ptr(dw_next), wp, wn)
+
+
+class W4Experts:
+    """SwiGLU experts with 4-bit weights, for batches of any size: tokens sorted by expert, the
+    experts' products over their rows, and the weighted way back.
+
+    gate, up and down are (codes, scale) pairs: gate and up [n, d, h / 2] and [n, d, h / group], down
+    [n, h, d / 2] and [n, h, d / group]."""
+
+    def __init__(self, gate, up, down):
+        self.gate, self.up, self.down = gate, up, down
+        self.n, self.d, half = gate[0].shape
+        self.h = 2 * half
+
+    def __call__(self, x, topk_ids, topk_w, y=None, stream=None):
+        """y [T, h] from x [T, h] (bf16), topk_ids [T, k] (int32, -1: none) and topk_w [T, k] (fp32)."""
+        if stream is not None:
+            with torch.cuda.stream(stream):
+                return self(x, topk_ids, topk_w, y)
+        T, k = topk_ids.shape
+        new, i32 = dict(device=x.device), torch.int32
+        offset, pair = torch.empty(self.n + 1, dtype=i32, **new), torch.empty(T * k, dtype=i32, **new)
+        row, xs = torch.empty(T, k, dtype=i32, **new), x.new_empty(T * k, self.h)
+        a, ys = x.new_empty(T * k, self.d), x.new_empty(T * k, self.h)
+        y = torch.empty_like(x) if y is None else y
+        deamoe_dispatch(topk_ids, x, offset, pair, row, xs)
+        deamoe_w4_swiglu(xs, *self.gate, *self.up, a, offset=offset)
+        deamoe_w4_linear(a, *self.down, ys, offset=offset)
+        deamoe_combine(row, topk_w, ys, y)
+        return y
+
+
+class Block:
+    """A layer between its norms: z = res_scale * x + gate * RMSNorm(layer(RMSNorm(x) * w_pre)) * w_post,
+    the layer being a Layer or any callable of the normed rows."""
+
+    def __init__(self, layer, w_pre, w_post, gate=None, res_scale: float = 1.0, eps: float = 1e-6,
+                 w_next=None):
+        self.layer, self.w_pre, self.w_post, self.gate = layer, w_pre, w_post, gate
+        self.res_scale, self.eps, self.w_next = res_scale, eps, w_next
+
+    def __call__(self, x, u=None, **kw):
+        """z, or with w_next (z, u): u is the next block's normed input, which its call takes in
+        place of norming x again.  Keyword arguments go to the layer."""
+        if u is None:
+            u = torch.empty_like(x)
+            deamoe_prenorm(x, self.w_pre, u, eps=self.eps)
+        y, z = self.layer(u, **kw), torch.empty_like(x)
+        nxt = torch.empty_like(x) if self.w_next is not None else None
+        deamoe_postnorm(x, y, self.w_post, z, gate=self.gate, res_scale=self.res_scale,
+                        w_next=self.w_next, u=nxt, eps=self.eps)
+        return z if nxt is None else (z, nxt)
