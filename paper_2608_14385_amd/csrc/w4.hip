@@ -49,110 +49,231 @@ __device__ inline void expert_rows(const W4Args &a, int e, int &lo, int &hi) {
   hi = min(max(a.offset[e + 1], lo), a.M);
 }
 
-// The matrix and the token rows of row tile `tile`, the tiles of `rows` rows
-// counted over the matrices in order.  False past the last.
-__device__ inline bool find_tile(const W4Args &a, int tile, int rows, int &e, int &m0, int &m1) {
+// The matrix e and the token rows [m0, m1) of tile `tile`, the tiles of `rows`
+// rows counted over the matrices in order.  False past the last.  Every wave
+// finds its tile by itself, with no barrier: a lane counts the tiles of a run
+// of matrices.
+__device__ inline bool find_tile(const W4Args &a, int64_t tile, int rows, int &e, int &m0,
+                                 int &m1) {
   if (!a.offset) {
     e = 0;
-    m0 = tile * rows;
+    if (tile * rows >= a.M) return false;
+    m0 = (int)tile * rows;
     m1 = min(m0 + rows, a.M);
-    return m0 < a.M;
+    return true;
   }
-  __shared__ int s_sum[kWaves], s_found[3];
-  __syncthreads();   // an earlier tile's s_found has been read
-  const int tid = threadIdx.x, lane = tid % kWave, wv = tid / kWave;
-  if (tid == 0) s_found[0] = -1;
-  int base = 0;
-  for (int e0 = 0; e0 < a.n && base <= tile; e0 += kThreads) {
-    int lo = 0, hi = 0;
-    if (e0 + tid < a.n) expert_rows(a, e0 + tid, lo, hi);
-    const int mine = (hi - lo + rows - 1) / rows;
-    int inc = mine;
-#pragma unroll
-    for (int d = 1; d < kWave; d *= 2) {
-      const int o = __shfl_up(inc, d);
-      inc += lane >= d ? o : 0;
-    }
-    __syncthreads();
-    if (lane == kWave - 1) s_sum[wv] = inc;
-    __syncthreads();
-    int at = base + inc - mine;
-#pragma unroll
-    for (int i = 0; i < kWaves; ++i) {
-      at += i < wv ? s_sum[i] : 0;
-      base += s_sum[i];
-    }
-    if (at <= tile && tile < at + mine) {
-      s_found[0] = e0 + tid;
-      s_found[1] = lo + (tile - at) * rows;
-      s_found[2] = hi;
-    }
+  const int lane = lane_id(), per = (a.n + kWave - 1) / kWave, e0 = min(lane * per, a.n);
+  const int e1 = min(e0 + per, a.n);
+  int mine = 0;
+  for (int i = e0; i < e1; ++i) {
+    int lo, hi;
+    expert_rows(a, i, lo, hi);
+    mine += (hi - lo + rows - 1) / rows;
   }
-  __syncthreads();
-  e = s_found[0];
-  m0 = s_found[1];
-  m1 = min(m0 + rows, s_found[2]);
-  return e >= 0;
+  int inc = mine;
+#pragma unroll
+  for (int d = 1; d < kWave; d *= 2) {
+    const int o = __shfl_up(inc, d);
+    inc += lane >= d ? o : 0;
+  }
+  const uint64_t past = __ballot(inc > tile);
+  if (!past) return false;
+  const int from = __ffsll((unsigned long long)past) - 1;   // the lane whose run holds the tile
+  int at = __builtin_amdgcn_readlane(inc - mine, from);
+  const int f0 = min(from * per, a.n), f1 = min(f0 + per, a.n);
+  for (int i = f0; i < f1; ++i) {
+    int lo, hi;
+    expert_rows(a, i, lo, hi);
+    const int t = (hi - lo + rows - 1) / rows;
+    if (tile < at + t) {
+      e = i;
+      m0 = lo + ((int)tile - at) * rows;
+      m1 = min(m0 + rows, hi);
+      return true;
+    }
+    at += t;
+  }
+  return false;   // not reached
 }
 
 __device__ inline float silu(float v) { return v / (1.0f + __expf(-v)); }
 
-// One wave: 16 token rows by 16 weight rows, over all columns.
-template <int MATS>
-__device__ inline void tile_product(const W4Args &a, int e, int m0, int m1, int r0) {
-  const int lane = lane_id(), j = lane & 15, g = lane >> 4;
-  const int r = min(r0 + j, a.R - 1), groups = a.K / a.group;
-  const char *x = static_cast<const char *>(a.x) + ((size_t)min(m0 + j, m1 - 1) * a.K + g * 8) * 2;
-  const size_t wrow = (size_t)e * a.R + r;
-  f32x4 acc[MATS] = {};
-  for (int q = 0; q < groups; ++q) {
-    f32x4 part[MATS];
-    f32x4 c0 = {0.f, 0.f, 0.f, 0.f};
-    for (int k = q * a.group; k < (q + 1) * a.group; k += 32)
-      c0 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-          order_columns(*reinterpret_cast<const u32x4 *>(x + k * 2)), minus_24(), c0, 0, 0, 0);
-    for (int n = 0; n < MATS; ++n) {
-      part[n] = c0;
-      for (int k = q * a.group; k < (q + 1) * a.group; k += 32) {
-        const uint32_t w = *reinterpret_cast<const uint32_t *>(
-            static_cast<const char *>(a.w[n]) + (wrow * a.K + k) / 2 + g * 4);
-        part[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-            order_columns(*reinterpret_cast<const u32x4 *>(x + k * 2)), codes_to_bf16(w), part[n],
-            0, 0, 0);
-      }
-      acc[n] += scale_at(a.scale[n], wrow * groups + q, a.scale_bf16) * part[n];
-    }
-  }
-  // lane (j, g) holds weight row r0 + j of tokens m0 + 4 g .. + 3
-  if (r0 + j >= a.R) return;
-  for (int i = 0; i < 4; ++i) {
-    const int m = m0 + g * 4 + i;
-    if (m >= m1) break;
-    const float v = MATS == 2 ? silu(acc[0][i]) * acc[MATS - 1][i] : acc[0][i];
-    static_cast<uint16_t *>(a.y)[(size_t)m * a.R + r0 + j] = f32_to_bf16(v);
-  }
+typedef __bf16 bf16;
+
+// Code dwords of 128 columns as loaded (dword m of lane group g: columns
+// 32 g + 8 m ...) -> dword m of lane group g: columns 32 m + 8 g ..., so that
+// one matrix product covers 32 columns that share a scale.
+__device__ inline void columns_together(u32x4 &v) {
+  auto s0 = __builtin_amdgcn_permlane32_swap(v[0], v[2], false, false);
+  auto s1 = __builtin_amdgcn_permlane32_swap(v[1], v[3], false, false);
+  auto t0 = __builtin_amdgcn_permlane16_swap(s0[0], s1[0], false, false);
+  auto t1 = __builtin_amdgcn_permlane16_swap(s0[1], s1[1], false, false);
+  v = u32x4{t0[0], t0[1], t1[0], t1[1]};
 }
 
 }  // namespace
 
-template <int MATS>
-__global__ __launch_bounds__(kThreads) void w4_kernel(W4Args a, int64_t items) {
-  const int rt = (a.R + kTile * kWaves - 1) / (kTile * kWaves);
+// Few token rows: the weights are streamed, each byte once per 16 * NTT rows.
+// A wave takes NR 16-row tiles of each matrix and every KS-th step of SC
+// columns; the loads of a step are requested together, a step ahead of its
+// products, straight into registers in operand order (16 rows of whole cache
+// lines).  Waves that share tiles add their sums over LDS at the end.
+template <int MATS, int NR, int NTT, int G32>
+__global__ __launch_bounds__(kThreads) void w4_stream_kernel(W4Args a, int64_t items, int ks) {
+  constexpr int SC = NTT > 2 ? 128 : 256, CH = SC / 128;   // columns of a step, 128 at a time
+  constexpr int NT = MATS * NR, SG = SC / 32 / G32;        // weight tiles, scales of a row
+  __shared__ f32x4 s_red[kWaves][NT][NTT][kWave];
+  const int lane = lane_id(), j = lane & 15, g = lane >> 4;
+  const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int parts = kWaves / ks, kp = wv % ks;   // row parts of the workgroup, this wave's K part
+  const int rows = parts * NR * kTile, rt = (a.R + rows - 1) / rows;
+  const int steps = (a.K + SC - 1) / SC, groups = a.K / (32 * G32);
   for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
     int e, m0, m1;
-    if (!find_tile(a, (int)(item / rt), kTile, e, m0, m1)) return;
-    const int r0 = ((int)(item % rt) * kWaves + threadIdx.x / kWave) * kTile;
-    if (r0 < a.R) tile_product<MATS>(a, e, m0, m1, r0);
+    if (!find_tile(a, item / rt, kTile * NTT, e, m0, m1)) return;
+    const int r0 = (int)(item % rt) * rows + (wv / ks) * NR * kTile;
+    const char *wp[NT];
+    size_t sp[NT];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      const size_t r = (size_t)e * a.R + min(r0 + (n % NR) * kTile + j, a.R - 1);
+      wp[n] = static_cast<const char *>(a.w[n / NR]) + r * (a.K / 2) + g * 16;
+      sp[n] = r * groups;
+    }
+    const char *xp[NTT];
+#pragma unroll
+    for (int t = 0; t < NTT; ++t)
+      xp[t] = static_cast<const char *>(a.x) +
+              ((size_t)min(m0 + t * kTile + j, m1 - 1) * a.K + g * 8) * 2;
+    u32x4 W[2][NT][CH], X[2][NTT][CH * 4];
+    float S[2][NT][SG];
+    auto request = [&](int q, int s) {
+      const int k0 = s * SC;
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+          const int k = k0 + c * 128;   // past the end: any codes, their x is 0
+          W[q][n][c] = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(
+              wp[n] + (k + g * 32 < a.K ? k / 2 : -g * 16)));
+        }
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int i = 0; i < SG; ++i) {
+          const int q0 = s * SG + i;
+          S[q][n][i] = q0 < groups ? scale_at(a.scale[n / NR], sp[n] + q0, a.scale_bf16) : 0.f;
+        }
+#pragma unroll
+      for (int t = 0; t < NTT; ++t)
+#pragma unroll
+        for (int b = 0; b < CH * 4; ++b) {
+          const int k = k0 + b * 32;
+          X[q][t][b] = u32x4{0, 0, 0, 0};
+          if (k < a.K) X[q][t][b] = *reinterpret_cast<const u32x4 *>(xp[t] + (size_t)k * 2);
+        }
+    };
+    f32x4 acc[NT][NTT] = {};
+    auto multiply = [&](int q) {
+#pragma unroll
+      for (int c = 0; c < CH; ++c) {
+        bf16x8 xb[NTT][4];
+#pragma unroll
+        for (int t = 0; t < NTT; ++t)
+#pragma unroll
+          for (int m = 0; m < 4; ++m) xb[t][m] = order_columns(X[q][t][c * 4 + m]);
+        f32x4 start[NTT][4 / G32];   // -24 sum(x) of every group
+#pragma unroll
+        for (int t = 0; t < NTT; ++t)
+#pragma unroll
+          for (int m = 0; m < 4; ++m) {
+            const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+            start[t][m / G32] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                xb[t][m], minus_24(), m % G32 ? start[t][m / G32] : zero, 0, 0, 0);
+          }
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+          columns_together(W[q][n][c]);
+          bf16x8 wb[4];
+#pragma unroll
+          for (int m = 0; m < 4; ++m) wb[m] = codes_to_bf16(W[q][n][c][m]);
+#pragma unroll
+          for (int t = 0; t < NTT; ++t)
+#pragma unroll
+            for (int i = 0; i < 4 / G32; ++i) {
+              f32x4 p = start[t][i];
+#pragma unroll
+              for (int m = 0; m < G32; ++m)
+                p = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xb[t][i * G32 + m], wb[i * G32 + m], p,
+                                                            0, 0, 0);
+              acc[n][t] += S[q][n][c * (4 / G32) + i] * p;
+            }
+        }
+      }
+    };
+    if (kp < steps) request(0, kp);
+    for (int s = kp; s < steps; s += 2 * ks) {
+      if (s + ks < steps) request(1, s + ks);
+      multiply(0);
+      if (s + ks >= steps) break;
+      if (s + 2 * ks < steps) request(0, s + 2 * ks);
+      multiply(1);
+    }
+    if (ks > 1) {
+      __syncthreads();   // the previous item's sums have been read
+      if (kp)
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int t = 0; t < NTT; ++t) s_red[wv][n][t][lane] = acc[n][t];
+      __syncthreads();
+      if (kp) continue;
+      for (int i = 1; i < ks; ++i)
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int t = 0; t < NTT; ++t) acc[n][t] += s_red[wv + i][n][t][lane];
+    }
+    // lane (j, g) holds weight row j of its tile for tokens 4 g .. 4 g + 3
+#pragma unroll
+    for (int n = 0; n < NR; ++n) {
+      const int r = r0 + n * kTile + j;
+#pragma unroll
+      for (int t = 0; t < NTT; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int m = m0 + t * kTile + g * 4 + i;
+          const float v = MATS == 2 ? silu(acc[n][t][i]) * acc[NT - NR + n][t][i] : acc[n][t][i];
+          if (r < a.R && m < m1)
+            reinterpret_cast<bf16 *>(a.y)[(size_t)m * a.R + r] = (bf16)v;
+        }
+    }
   }
 }
 
-hipError_t launch_w4(const W4Args &a, int mats, hipStream_t s) {
-  const int64_t tiles = a.M / kTile + (a.offset ? (a.n < a.M ? a.n : a.M) : 1);   // the most there can be
-  const int64_t items = tiles * ((a.R + kTile * kWaves - 1) / (kTile * kWaves));
-  const dim3 grid((unsigned)(items < (1 << 20) ? items : 1 << 20));
-  if (mats == 2) hipLaunchKernelGGL(w4_kernel<2>, grid, dim3(kThreads), 0, s, a, items);
-  else hipLaunchKernelGGL(w4_kernel<1>, grid, dim3(kThreads), 0, s, a, items);
+namespace {
+
+template <int MATS, int NR, int NTT>
+hipError_t stream_grouped(const W4Args &a, int ks, hipStream_t s) {
+  const int tr = kTile * NTT, rows = kWaves / ks * NR * kTile;
+  const int64_t tiles = a.offset ? a.M / tr + (a.n < a.M ? a.n : a.M) : (a.M + tr - 1) / tr;
+  const int64_t items = tiles * ((a.R + rows - 1) / rows);   // the most there can be
+  const dim3 grid((unsigned)(items < (1 << 20) ? items : 1 << 20)), block(kThreads);
+  if (a.group == 32)
+    hipLaunchKernelGGL((w4_stream_kernel<MATS, NR, NTT, 1>), grid, block, 0, s, a, items, ks);
+  else if (a.group == 64)
+    hipLaunchKernelGGL((w4_stream_kernel<MATS, NR, NTT, 2>), grid, block, 0, s, a, items, ks);
+  else
+    hipLaunchKernelGGL((w4_stream_kernel<MATS, NR, NTT, 4>), grid, block, 0, s, a, items, ks);
   return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_w4(const W4Args &a, int mats, hipStream_t s) {
+  const int per = a.offset ? (a.M + a.n - 1) / a.n : a.M;   // rows of a matrix on average
+  if (mats == 2) return per <= 16 ? stream_grouped<2, 1, 1>(a, 4, s) : stream_grouped<2, 1, 2>(a, 4, s);
+  return per <= 16 ? stream_grouped<1, 1, 1>(a, 4, s) : stream_grouped<1, 1, 4>(a, 4, s);
 }
 
 }  // namespace deamoe
