@@ -47,60 +47,72 @@ __device__ inline bf16x8 minus_24() {
   return __builtin_bit_cast(bf16x8, r);
 }
 
-__device__ inline float scale_at(const void *p, size_t i, int bf16) {
-  return bf16 ? bf16_to_f32(static_cast<const uint16_t *>(p)[i]) : static_cast<const float *>(p)[i];
-}
+// The row tiles of all matrices, `rows` rows each, counted over the matrices in
+// order.  Every wave counts and finds tiles by itself, with no barrier: a lane
+// counts the tiles of a run of matrices.  Offsets outside [0, M] count as the
+// nearer end.
+struct Tiles {
+  int rows, per, mine, inc;   // matrices of a lane's run, its tiles, those up to its end
+  int total;
 
-// The matrix e and the token rows [m0, m1) of tile `tile`, the tiles of `rows`
-// rows counted over the matrices in order.  False past the last.  Every wave
-// finds its tile by itself, with no barrier: a lane counts the tiles of a run
-// of matrices.  Offsets outside [0, M] count as the nearer end.
-__device__ inline bool find_tile(const W4Args &a, int64_t tile, int rows, int &e, int &m0,
-                                 int &m1) {
-  if (!a.offset) {
-    e = 0;
-    if (tile * rows >= a.M) return false;
-    m0 = (int)tile * rows;
-    m1 = min(m0 + rows, a.M);
-    return true;
-  }
-  const int lane = lane_id(), per = (a.n + kWave - 1) / kWave, e0 = lane * per;
-  constexpr int U = 4;   // offsets read at once
-  int mine = 0;
-  for (int i = 0; i < per; i += U) {
-    int o[U + 1];
+  __device__ Tiles(const W4Args &a, int rows_) : rows(rows_) {
+    if (!a.offset) {
+      total = (a.M + rows - 1) / rows;
+      return;
+    }
+    const int lane = lane_id(), e0 = lane * (per = (a.n + kWave - 1) / kWave);
+    constexpr int U = 4;   // offsets read at once
+    mine = 0;
+    for (int i = 0; i < per; i += U) {
+      int o[U + 1];
 #pragma unroll
-    for (int u = 0; u <= U; ++u) o[u] = min(max(a.offset[min(e0 + min(i + u, per), a.n)], 0), a.M);
+      for (int u = 0; u <= U; ++u) o[u] = clamped(a, e0 + min(i + u, per));
 #pragma unroll
-    for (int u = 0; u < U; ++u) mine += (max(o[u + 1] - o[u], 0) + rows - 1) / rows;
+      for (int u = 0; u < U; ++u) mine += (max(o[u + 1] - o[u], 0) + rows - 1) / rows;
+    }
+    inc = mine;
+    scan<kWave>(inc);
+    total = __builtin_amdgcn_readlane(inc, kWave - 1);
   }
-  int inc = mine;
+
+  // Matrix and token rows [m0, m1) of a tile below `total`.
+  __device__ void find(const W4Args &a, int tile, int &e, int &m0, int &m1) const {
+    if (!a.offset) {
+      e = 0;
+      m0 = tile * rows;
+      m1 = min(m0 + rows, a.M);
+      return;
+    }
+    const int lane = lane_id();
+    const int from = first(inc > tile);   // the lane whose run holds the tile
+    // the lanes look at the matrices of that run: DEAMOE_MAX_EXPERTS / 64 at most
+    const int base = __builtin_amdgcn_readlane(inc - mine, from), f = from * per + lane;
+    const int lo = clamped(a, f), hi = max(clamped(a, f + 1), lo);
+    const int here = lane < per && f < a.n ? (hi - lo + rows - 1) / rows : 0;
+    int upto = here;
+    scan<DEAMOE_MAX_EXPERTS / kWave>(upto);
+    const int at = first(base + upto > tile);
+    e = from * per + at;
+    m0 = __builtin_amdgcn_readlane(lo, at) +
+         (tile - base - __builtin_amdgcn_readlane(upto - here, at)) * rows;
+    m1 = min(m0 + rows, __builtin_amdgcn_readlane(hi, at));
+  }
+
+ private:
+  __device__ static int clamped(const W4Args &a, int e) {
+    return min(max(a.offset[min(e, a.n)], 0), a.M);
+  }
+  __device__ static int first(bool v) { return __ffsll((unsigned long long)__ballot(v)) - 1; }
+  template <int LANES>
+  __device__ static void scan(int &v) {   // inclusive, over the first LANES lanes
+    const int lane = lane_id();
 #pragma unroll
-  for (int d = 1; d < kWave; d *= 2) {
-    const int o = __shfl_up(inc, d);
-    inc += lane >= d ? o : 0;
+    for (int d = 1; d < LANES; d *= 2) {
+      const int o = __shfl_up(v, d);
+      v += lane >= d ? o : 0;
+    }
   }
-  const uint64_t past = __ballot(inc > tile);
-  if (!past) return false;
-  const int from = __ffsll((unsigned long long)past) - 1;   // the lane whose run holds the tile
-  // the lanes look at the matrices of that run, 64 at most (DEAMOE_MAX_EXPERTS / 64 are fewer)
-  const int base = __builtin_amdgcn_readlane(inc - mine, from), f = from * per + lane;
-  const int lo = min(max(a.offset[min(f, a.n)], 0), a.M);
-  const int hi = max(min(max(a.offset[min(f + 1, a.n)], 0), a.M), lo);
-  const int here = lane < per && f < a.n ? (hi - lo + rows - 1) / rows : 0;
-  inc = here;
-#pragma unroll
-  for (int d = 1; d < DEAMOE_MAX_EXPERTS / kWave; d *= 2) {
-    const int o = __shfl_up(inc, d);
-    inc += lane >= d ? o : 0;
-  }
-  const int at = __ffsll((unsigned long long)__ballot(base + inc > tile)) - 1;
-  e = from * per + at;
-  m0 = __builtin_amdgcn_readlane(lo, at) +
-       ((int)tile - base - __builtin_amdgcn_readlane(inc - here, at)) * rows;
-  m1 = min(m0 + rows, __builtin_amdgcn_readlane(hi, at));
-  return true;
-}
+};
 
 // A pointer every lane holds alike, in scalar registers.
 template <class P>
@@ -114,6 +126,11 @@ __device__ inline float silu(float v) { return v / (1.0f + __expf(-v)); }
 
 typedef __bf16 bf16;
 
+template <int CTRL>
+__device__ inline float dpp(float v) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, false));
+}
+
 // Code dwords of 128 columns as loaded (dword m of lane group g: columns
 // 32 g + 8 m ...) -> dword m of lane group g: columns 32 m + 8 g ..., so that
 // one matrix product covers 32 columns that share a scale.
@@ -123,6 +140,26 @@ __device__ inline void columns_together(u32x4 &v) {
   auto t0 = __builtin_amdgcn_permlane16_swap(s0[0], s1[0], false, false);
   auto t1 = __builtin_amdgcn_permlane16_swap(s0[1], s1[1], false, false);
   v = u32x4{t0[0], t0[1], t1[0], t1[1]};
+}
+
+// -24 times the sum of the eight columns of x held by each lane and by its
+// neighbours in runs of LANES (4, 8 or 16), in fp32.
+template <int LANES>
+__device__ inline float minus_24_sum(u32x4 v) {
+  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+  const bf16x2 c = {(__bf16)-24.f, (__bf16)-24.f};
+  float s = 0.f;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t pair = v[i];   // a bit cast of the element itself would take element 0
+    s = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pair), c, s, false);
+  }
+  // lane i adds lane i ^ 1, i ^ 2, then a lane of the other quad, of the other half row
+  s += dpp<0xb1>(s);
+  s += dpp<0x4e>(s);
+  if constexpr (LANES > 4) s += dpp<0x141>(s);
+  if constexpr (LANES > 8) s += dpp<0x140>(s);
+  return s;
 }
 
 // Codes of 256 columns of 16 rows as loaded: a of rows 0 to 7 and b of rows 8 to
@@ -158,7 +195,7 @@ constexpr int kPanelWords = 16 * (1024 + 8) / 2;   // of a token tile, 4 bytes e
 constexpr int kPanelScales = 32;                   // of a weight row, at most
 constexpr int kNonTemporal = 2;                    // cache policy of a buffer load
 template <int MATS, int NR, int NTT, int G32, bool SBF, int D, int CH>
-__global__ __launch_bounds__(kThreads, 2) void w4_stream_kernel(W4Args a, int64_t items, int ks) {
+__global__ __launch_bounds__(kThreads, 2) void w4_stream_kernel(W4Args a, int ks) {
   constexpr int SC = 128 * CH, NT = MATS * NR, GS = 32 * G32;
   constexpr int TR = NTT * kTile, WORDS = kPanelWords * NTT;
   __shared__ __align__(16) uint32_t s_x[WORDS];
@@ -170,9 +207,11 @@ __global__ __launch_bounds__(kThreads, 2) void w4_stream_kernel(W4Args a, int64_
   const int wv = uniform(tid / kWave);
   const int kp = wv % ks, rows = kWaves / ks * NR * kTile, rt = (a.R + rows - 1) / rows;
   const int steps = (a.K + SC - 1) / SC, groups = a.K / GS;
+  const Tiles tiles(a, TR);
+  const int64_t items = (int64_t)uniform(tiles.total) * rt;
   for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
     int e, m0, m1;
-    if (!uniform(find_tile(a, item / rt, TR, e, m0, m1))) return;
+    tiles.find(a, (int)(item / rt), e, m0, m1);
     e = uniform(e), m0 = uniform(m0);
     const int ntok = uniform(m1) - m0;
     const int r0 = uniform((int)(item % rt) * rows + (wv / ks) * NR * kTile);
@@ -306,6 +345,7 @@ __global__ __launch_bounds__(kThreads, 2) void w4_stream_kernel(W4Args a, int64_
       __syncthreads();
       const int end = min(p0 + pcol, a.K);
       auto steps_of_panel = [&] {
+#pragma unroll 1
         for (int s = p0 / SC + kp;; s += D * ks)
 #pragma unroll
           for (int d = 0; d < D; ++d) {
@@ -350,6 +390,192 @@ __global__ __launch_bounds__(kThreads, 2) void w4_stream_kernel(W4Args a, int64_
   }
 }
 
+// Many token rows: a workgroup multiplies 64 of them with 256 weight rows (with
+// two matrices 128 of each), every wave 64 rows of its own, so that no code is
+// unpacked twice and a token row read from LDS meets four weight tiles.  The
+// -24 sums are made once, by the threads that bring the token rows to LDS.
+// Both operands of the next step are requested before a step's products; the
+// token rows go through registers, where they take the codes' order, into the
+// other half of the LDS buffer.
+constexpr int kTileTok = 64, kTileStep = 128, kTileStride = kTileStep + 8;
+template <int MATS, int G32, bool SBF>
+__global__ __launch_bounds__(kThreads, 2) void w4_tile_kernel(W4Args a) {
+  constexpr int NT = 4, NR = NT / MATS, NTT = kTileTok / kTile, GS = 32 * G32;
+  constexpr int XC = kTileTok * kTileStep / 8 / kThreads;   // 16-byte chunks of x per thread
+  __shared__ __align__(16) uint16_t s_x[2][kTileTok][kTileStride];
+  __shared__ __align__(16) float s_start[2][4 / G32][kTileTok];
+  __shared__ float s_scale[kWaves][NT][kTile][kPanelScales + 1];
+  const int lane = lane_id(), j = lane & 15, g = lane >> 4, tid = threadIdx.x;
+  const int wv = uniform(tid / kWave);
+  const int rows = kWaves * NR * kTile, rt = (a.R + rows - 1) / rows;
+  const int steps = (a.K + kTileStep - 1) / kTileStep, groups = a.K / GS;
+  const Tiles tiles(a, kTileTok);
+  // Consecutive workgroups run on the 8 XCDs in turn: each XCD gets a run of
+  // neighbouring items, which share weights and token rows in its L2.
+  const int64_t items = (int64_t)uniform(tiles.total) * rt, run = (items + 7) / 8;
+  for (int64_t i = blockIdx.x / 8; i < run; i += gridDim.x / 8) {
+    const int64_t item = blockIdx.x % 8 * run + i;
+    if (item >= items) return;
+    int e, m0, m1;
+    tiles.find(a, (int)(item / rt), e, m0, m1);
+    e = uniform(e), m0 = uniform(m0);
+    const int ntok = uniform(m1) - m0;
+    const int r0 = uniform((int)(item % rt) * rows + wv * NR * kTile);
+    const int left = max(a.R - r0, 1);   // a wave past the last row repeats it
+    const size_t first = (size_t)e * a.R + min(r0, a.R - 1);
+    const uint32_t wrow = a.K / 2;
+    char *wb[MATS];
+    const void *sb[MATS];
+#pragma unroll
+    for (int n = 0; n < MATS; ++n) {
+      wb[n] = const_cast<char *>(uniform_ptr(static_cast<const char *>(a.w[n]) + first * wrow));
+      sb[n] = uniform_ptr(static_cast<const char *>(a.scale[n]) + first * groups * (SBF ? 2 : 4));
+    }
+    uint32_t wo[NR];
+#pragma unroll
+    for (int n = 0; n < NR; ++n) wo[n] = (n * kTile + j) * wrow + g * 16;
+    char *xb = const_cast<char *>(
+        uniform_ptr(static_cast<const char *>(a.x) + (size_t)m0 * a.K * 2));
+    uint32_t xo[XC];   // token row tid / 16 + 16 i, chunk tid % 16
+#pragma unroll
+    for (int i = 0; i < XC; ++i)
+      xo[i] = (uint32_t)min(tid / 16 + i * 16, ntok - 1) * a.K * 2 + tid % 16 * 16;
+    u32x4 W[2][NT], X[XC];
+    auto request_w = [&](int q, int s) {
+      const int bytes = s < steps ? (int)(left * wrow) : 0, at = s < steps ? s * (kTileStep / 2) : 0;
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+        W[q][n] = __builtin_amdgcn_raw_buffer_load_b128(
+            __builtin_amdgcn_make_buffer_rsrc(wb[n / NR], 0, bytes, 0x00027000), wo[n % NR], at, 0);
+    };
+    auto request_x = [&](int s) {
+      const bool ok = s * kTileStep + tid % 16 * 8 < a.K;
+#pragma unroll
+      for (int i = 0; i < XC; ++i)
+        X[i] = *gptr(xb + xo[i] + (ok ? (uint32_t)s * kTileStep * 2 : 0u));
+    };
+    auto put_x = [&](int q, int s) {
+      const bool ok = s * kTileStep + tid % 16 * 8 < a.K;
+#pragma unroll
+      for (int i = 0; i < XC; ++i) {
+        const u32x4 v = ok ? X[i] : u32x4{0, 0, 0, 0};
+        const int row = tid / 16 + i * 16;
+        *reinterpret_cast<bf16x8 *>(&s_x[q][row][tid % 16 * 8]) = order_columns(v);
+        const float sum = minus_24_sum<G32 * 4>(v);
+        if (tid % (G32 * 4) == 0) s_start[q][tid % 16 / (G32 * 4)][row] = sum;
+      }
+    };
+    auto put_scales = [&](int q0) {   // this wave's, of kPanelScales groups
+#pragma unroll 1
+      for (int n = 0; n < NT; ++n) {
+        constexpr int N = kTile * kPanelScales / kWave;
+        const void *from = n < NR ? sb[0] : sb[MATS - 1];
+        float v[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) {   // two rows at a time
+          const int r = n % NR * kTile + i * 2 + lane / kPanelScales, q = q0 + lane % kPanelScales;
+          const bool ok = q < groups && r < left;
+          const uint32_t at = ok ? r * groups + q : 0;
+          if constexpr (SBF) v[i] = bf16_to_f32(glob(static_cast<const uint16_t *>(from))[at]);
+          else v[i] = glob(static_cast<const float *>(from))[at];
+          v[i] = ok ? v[i] : 0.f;
+        }
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+          s_scale[wv][n][i * 2 + lane / kPanelScales][lane % kPanelScales] = v[i];
+      }
+    };
+    f32x4 acc[NT][NTT] = {};
+    const Magic magic;
+    auto multiply = [&](int q, int s) {
+      const int q0 = s * (4 / G32) % kPanelScales;
+#pragma unroll
+      for (int n = 0; n < NT; ++n) columns_together(W[q][n]);
+#pragma unroll
+      for (int i = 0; i < 4 / G32; ++i) {
+        // The shortest groups take two token tiles at a time, whose sums and the
+        // group's unpacked weights fit the registers beside acc.
+        constexpr int TP = G32 == 1 ? 2 : NTT;
+        bf16x8 w[NT];
+        if constexpr (G32 == 1)
+#pragma unroll
+          for (int n = 0; n < NT; ++n) w[n] = codes_to_bf16(W[q][n][i], magic);
+#pragma unroll
+        for (int t0 = 0; t0 < NTT; t0 += TP) {
+          f32x4 p[NT][TP];
+#pragma unroll
+          for (int t = 0; t < TP; ++t) {   // lane group g: tokens 4 g .. 4 g + 3 of the tile
+            p[0][t] = *reinterpret_cast<const f32x4 *>(&s_start[q][i][(t0 + t) * kTile + g * 4]);
+#pragma unroll
+            for (int n = 1; n < NT; ++n) p[n][t] = p[0][t];
+          }
+#pragma unroll
+          for (int m = 0; m < G32; ++m) {
+            bf16x8 xv[TP];
+#pragma unroll
+            for (int t = 0; t < TP; ++t)
+              xv[t] = *reinterpret_cast<const bf16x8 *>(
+                  &s_x[q][(t0 + t) * kTile + j][(i * G32 + m) * 32 + g * 8]);
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+              if constexpr (G32 > 1) w[n] = codes_to_bf16(W[q][n][i * G32 + m], magic);
+#pragma unroll
+              for (int t = 0; t < TP; ++t)
+                p[n][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xv[t], w[n], p[n][t], 0, 0, 0);
+            }
+          }
+#pragma unroll
+          for (int n = 0; n < NT; ++n) {
+            const float sc = s_scale[wv][n][j][q0 + i];
+#pragma unroll
+            for (int t = 0; t < TP; ++t) {
+              acc[n][t0 + t] += sc * p[n][t];
+              // here and now: left to the end of the step, all groups' sums
+              // would have to be kept
+              asm volatile("" : "+v"(acc[n][t0 + t]));
+            }
+          }
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      }
+    };
+    __syncthreads();   // the last item's token rows have been read
+    request_w(0, 0);
+    request_x(0);
+    put_scales(0);
+    put_x(0, 0);
+    __syncthreads();
+    auto all_steps = [&] {
+#pragma unroll 1
+      for (int s = 0;; s += 2)
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+          if (s + q >= steps) return;
+          request_x(s + q + 1);
+          request_w(q ^ 1, s + q + 1);
+          multiply(q, s + q);
+          if ((s + q + 1) * (4 / G32) % kPanelScales == 0) put_scales((s + q + 1) * (4 / G32));
+          put_x(q ^ 1, s + q + 1);
+          __syncthreads();
+        }
+    };
+    all_steps();
+#pragma unroll
+    for (int n = 0; n < NR; ++n) {
+      const int r = r0 + n * kTile + j;
+#pragma unroll
+      for (int t = 0; t < NTT; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int m = t * kTile + g * 4 + i;
+          const float v = MATS == 2 ? silu(acc[n][t][i]) * acc[NT - NR + n][t][i] : acc[n][t][i];
+          if (r < a.R && m < ntok)
+            reinterpret_cast<bf16 *>(a.y)[(size_t)(m0 + m) * a.R + r] = (bf16)v;
+        }
+    }
+  }
+}
+
 namespace {
 
 // K parts of a workgroup, at most `want`: a panel holds a round of the ring.
@@ -368,8 +594,8 @@ hipError_t stream_grouped(const W4Args &a, int want, hipStream_t s) {
   const int64_t tiles = a.offset ? a.M / tr + (a.n < a.M ? a.n : a.M) : (a.M + tr - 1) / tr;
   const int64_t items = tiles * ((a.R + rows - 1) / rows);   // the most there can be
   const dim3 grid((unsigned)(items < (1 << 20) ? items : 1 << 20)), block(kThreads);
-#define W4_STREAM(G, B)                                                                         \
-  hipLaunchKernelGGL((w4_stream_kernel<MATS, NR, NTT, G, B, D, CH>), grid, block, 0, s, a, items, ks)
+#define W4_STREAM(G, B) \
+  hipLaunchKernelGGL((w4_stream_kernel<MATS, NR, NTT, G, B, D, CH>), grid, block, 0, s, a, ks)
   if (a.scale_bf16) {
     if (a.group == 32) W4_STREAM(1, true);
     else if (a.group == 64) W4_STREAM(2, true);
@@ -383,11 +609,32 @@ hipError_t stream_grouped(const W4Args &a, int want, hipStream_t s) {
   return hipGetLastError();
 }
 
+template <int MATS>
+hipError_t tile_grouped(const W4Args &a, hipStream_t s) {
+  const int rows = kWaves * 4 / MATS * kTile;
+  const int64_t tiles = a.offset ? a.M / kTileTok + (a.n < a.M ? a.n : a.M) : (a.M + kTileTok - 1) / kTileTok;
+  const int64_t items = (tiles * ((a.R + rows - 1) / rows) + 7) / 8 * 8;   // the most there can be
+  const dim3 grid((unsigned)(items < (1 << 20) ? items : 1 << 20)), block(kThreads);
+#define W4_TILE(G, B) hipLaunchKernelGGL((w4_tile_kernel<MATS, G, B>), grid, block, 0, s, a)
+  if (a.scale_bf16) {
+    if (a.group == 32) W4_TILE(1, true);
+    else if (a.group == 64) W4_TILE(2, true);
+    else W4_TILE(4, true);
+  } else {
+    if (a.group == 32) W4_TILE(1, false);
+    else if (a.group == 64) W4_TILE(2, false);
+    else W4_TILE(4, false);
+  }
+#undef W4_TILE
+  return hipGetLastError();
+}
+
 }  // namespace
 
 hipError_t launch_w4(const W4Args &a, int mats, hipStream_t s) {
   const int per = a.offset ? (a.M + a.n - 1) / a.n : a.M;   // rows of a matrix on average
   const int ks = a.offset ? 1 : 4;
+  if (per > 64) return mats == 2 ? tile_grouped<2>(a, s) : tile_grouped<1>(a, s);
   if (mats == 2)
     return per <= 16 ? stream_grouped<2, 1, 1, 2, 2>(a, ks, s) : stream_grouped<2, 1, 2, 2, 2>(a, ks, s);
   return per <= 16 ? stream_grouped<1, 1, 1, 2, 2>(a, ks, s) : stream_grouped<1, 1, 4, 2, 2>(a, ks, s);
