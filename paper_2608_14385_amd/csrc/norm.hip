@@ -84,8 +84,8 @@ __device__ inline float rms_factor(float sum, int h, float eps) {
 
 // u = x^ w of one row.
 template <bool F32, int N>
-__device__ inline void norm_row(const Row<F32, N> &x, const void *w, char *u, int h, float eps,
-                                Reduce &red) {
+__device__ inline void norm_row(const Row<F32, N> &x, const Row<F32, N> &w, char *u, int h,
+                                float eps, Reduce &red) {
   constexpr int V = kVec<F32>;
   float ss[1] = {0.f};
   chunks<F32, N>(h, [&](int i, int c) {
@@ -96,7 +96,7 @@ __device__ inline void norm_row(const Row<F32, N> &x, const void *w, char *u, in
   red.sum(ss);
   const float r = rms_factor(ss[0], h, eps);
   chunks<F32, N>(h, [&](int i, int c) {
-    const Chunk<F32> v = x.get(i, c), g = load_chunk<F32>(w, c, h);
+    const Chunk<F32> v = x.get(i, c), g = w.get(i, c);
     float o[V];
 #pragma unroll
     for (int e = 0; e < V; ++e) o[e] = v.at(e) * r * g.at(e);
@@ -111,8 +111,8 @@ __global__ __launch_bounds__(MAXG) void prenorm_kernel(PrenormArgs a) {
   __shared__ float s_red[2][kMaxSums][kMaxWaves];
   Reduce red{s_red};
   for (int t = blockIdx.x; t < a.T; t += gridDim.x) {
-    const Row<F32, N> x(a.x, t, a.h);
-    norm_row<F32, N>(x, a.w, row_at<F32>(a.u, t, a.h), a.h, a.eps, red);
+    const Row<F32, N> x(a.x, t, a.h), w(a.w, 0, a.h);
+    norm_row<F32, N>(x, w, row_at<F32>(a.u, t, a.h), a.h, a.eps, red);
   }
 }
 
@@ -122,7 +122,10 @@ __global__ __launch_bounds__(MAXG) void postnorm_kernel(PostnormArgs a) {
   __shared__ float s_red[2][kMaxSums][kMaxWaves];
   Reduce red{s_red};
   for (int t = blockIdx.x; t < a.T; t += gridDim.x) {
-    const Row<F32, N> y(a.y, t, a.h), x(a.x, t, a.h);
+    // all of the row's loads before the first sum is waited for
+    const Row<F32, N> y(a.y, t, a.h), x(a.x, t, a.h), w(a.w, 0, a.h);
+    const Row<F32, N> gate(a.gate_mode ? a.gate : a.w, a.gate_mode == DEAMOE_GATE_FULL ? t : 0, a.h);
+    const Row<F32, N> w_next(a.u ? a.w_next : a.w, 0, a.h);
     float ss[1] = {0.f};
     chunks<F32, N>(a.h, [&](int i, int c) {
       const Chunk<F32> v = y.get(i, c);
@@ -131,17 +134,16 @@ __global__ __launch_bounds__(MAXG) void postnorm_kernel(PostnormArgs a) {
     });
     red.sum(ss);
     const float r = rms_factor(ss[0], a.h, a.eps);
-    const char *gate = row_at<F32>(a.gate, a.gate_mode == DEAMOE_GATE_FULL ? t : 0, a.h);
     char *zp = row_at<F32>(a.z, t, a.h);
     Row<F32, N> z = x;
     z.p = zp;
     chunks<F32, N>(a.h, [&](int i, int c) {
-      const Chunk<F32> yv = y.get(i, c), xv = x.get(i, c), w = load_chunk<F32>(a.w, c, a.h);
+      const Chunk<F32> yv = y.get(i, c), xv = x.get(i, c), wv = w.get(i, c);
       float o[V];
 #pragma unroll
-      for (int e = 0; e < V; ++e) o[e] = yv.at(e) * r * w.at(e);
+      for (int e = 0; e < V; ++e) o[e] = yv.at(e) * r * wv.at(e);
       if (a.gate_mode != DEAMOE_GATE_NONE) {
-        const Chunk<F32> g = load_chunk<F32>(gate, c, a.h);
+        const Chunk<F32> g = gate.get(i, c);
 #pragma unroll
         for (int e = 0; e < V; ++e) o[e] *= g.at(e);
       }
@@ -150,7 +152,7 @@ __global__ __launch_bounds__(MAXG) void postnorm_kernel(PostnormArgs a) {
       z.held[i] = pack_chunk<F32>(o);   // past the row's end: zeros, as loaded
       store_chunk<F32>(zp, c, a.h, z.held[i]);
     });
-    if (a.u) norm_row<F32, N>(z, a.w_next, row_at<F32>(a.u, t, a.h), a.h, a.eps, red);
+    if (a.u) norm_row<F32, N>(z, w_next, row_at<F32>(a.u, t, a.h), a.h, a.eps, red);
   }
 }
 
@@ -159,6 +161,17 @@ __global__ __launch_bounds__(MAXG) void postnorm_kernel(PostnormArgs a) {
 // t + grid, ... and keeps its sums over them for its columns: in registers, or
 // for wide rows in its part of the workspace.
 enum NormMode : int { NORM_PRE = 0, NORM_POST = 1, NORM_BOTH = 2 };
+
+template <bool F32, int N, int MODE>
+struct BackwardRows {   // what one row reads
+  Row<F32, MODE != NORM_POST ? N : 0> z, du;
+  Row<F32, MODE != NORM_PRE ? N : 0> y;
+  Row<F32, N> dz, gate;
+  __device__ BackwardRows(const NormBackwardArgs &a, int t)
+      : z(a.z, t, a.h), du(a.du, t, a.h), y(a.y, t, a.h), dz(a.dz ? a.dz : a.du, t, a.h),
+        gate(a.gate_mode == DEAMOE_GATE_NONE ? (a.w ? a.w : a.w_next) : a.gate,
+             a.gate_mode == DEAMOE_GATE_FULL ? t : 0, a.h) {}
+};
 
 template <bool F32, int N, int MAXG, int MODE>
 __global__ __launch_bounds__(MAXG) void norm_backward_kernel(NormBackwardArgs a) {
@@ -181,22 +194,26 @@ __global__ __launch_bounds__(MAXG) void norm_backward_kernel(NormBackwardArgs a)
         }
     }
   };
+  const Row<F32, POST ? N : 0> w(a.w, 0, h);
+  const Row<F32, NEXT ? N : 0> w_next(a.w_next, 0, h);
+  BackwardRows<F32, N, MODE> next(a, blockIdx.x);
   for (int t = blockIdx.x; t < a.T; t += gridDim.x) {
     const bool first = t == (int)blockIdx.x;
-    const Row<F32, NEXT ? N : 0> z(a.z, t, h), du(a.du, t, h);
-    const Row<F32, POST ? N : 0> y(a.y, t, h);
+    const BackwardRows<F32, N, MODE> r = next;
+    // the next row is on its way while this one waits for its sums
+    if (t + (int)gridDim.x < a.T) next = BackwardRows<F32, N, MODE>(a, t + gridDim.x);
     float s1[3] = {0.f, 0.f, 0.f};   // z^2, du w' z, y^2
     chunks<F32, N>(h, [&](int i, int c) {
       if constexpr (NEXT) {
-        const Chunk<F32> zv = z.get(i, c), g = du.get(i, c), w = load_chunk<F32>(a.w_next, c, h);
+        const Chunk<F32> zv = r.z.get(i, c), g = r.du.get(i, c), wv = w_next.get(i, c);
 #pragma unroll
         for (int e = 0; e < V; ++e) {
           s1[0] = __builtin_fmaf(zv.at(e), zv.at(e), s1[0]);
-          s1[1] = __builtin_fmaf(g.at(e) * w.at(e), zv.at(e), s1[1]);
+          s1[1] = __builtin_fmaf(g.at(e) * wv.at(e), zv.at(e), s1[1]);
         }
       }
       if constexpr (POST) {
-        const Chunk<F32> yv = y.get(i, c);
+        const Chunk<F32> yv = r.y.get(i, c);
 #pragma unroll
         for (int e = 0; e < V; ++e) s1[2] = __builtin_fmaf(yv.at(e), yv.at(e), s1[2]);
       }
@@ -206,36 +223,31 @@ __global__ __launch_bounds__(MAXG) void norm_backward_kernel(NormBackwardArgs a)
     const float ry = rms_factor(s1[2], h, a.eps);
     // d of one chunk: the gradient that reaches z
     auto reach = [&](int i, int c, float (&d)[V]) {
+      const Chunk<F32> v = r.dz.get(i, c);
 #pragma unroll
-      for (int e = 0; e < V; ++e) d[e] = 0.f;
-      if (a.dz) {
-        const Chunk<F32> v = load_chunk<F32>(row_at<F32>(a.dz, t, h), c, h);
-#pragma unroll
-        for (int e = 0; e < V; ++e) d[e] = v.at(e);
-      }
+      for (int e = 0; e < V; ++e) d[e] = a.dz ? v.at(e) : 0.f;
       if constexpr (NEXT) {
-        const Chunk<F32> zv = z.get(i, c), g = du.get(i, c), w = load_chunk<F32>(a.w_next, c, h);
+        const Chunk<F32> zv = r.z.get(i, c), g = r.du.get(i, c), wv = w_next.get(i, c);
 #pragma unroll
-        for (int e = 0; e < V; ++e) d[e] += rz * (g.at(e) * w.at(e) - zv.at(e) * rz * mz);
+        for (int e = 0; e < V; ++e) d[e] += rz * (g.at(e) * wv.at(e) - zv.at(e) * rz * mz);
       }
     };
-    const char *gate = row_at<F32>(a.gate, a.gate_mode == DEAMOE_GATE_FULL ? t : 0, h);
     float dh[NH][V];   // d of every held chunk
     float s2[1] = {0.f};
     chunks<F32, N>(h, [&](int i, int c) {
       reach(i, c, dh[i]);
       if constexpr (POST) {
-        const Chunk<F32> yv = y.get(i, c), w = load_chunk<F32>(a.w, c, h);
+        const Chunk<F32> yv = r.y.get(i, c), wv = w.get(i, c);
         float dn[V];
 #pragma unroll
         for (int e = 0; e < V; ++e) dn[e] = dh[i][e];
         if (a.gate_mode != DEAMOE_GATE_NONE) {
-          const Chunk<F32> g = load_chunk<F32>(gate, c, h);
+          const Chunk<F32> g = r.gate.get(i, c);
 #pragma unroll
           for (int e = 0; e < V; ++e) dn[e] *= g.at(e);
         }
 #pragma unroll
-        for (int e = 0; e < V; ++e) s2[0] = __builtin_fmaf(dn[e] * w.at(e), yv.at(e) * ry, s2[0]);
+        for (int e = 0; e < V; ++e) s2[0] = __builtin_fmaf(dn[e] * wv.at(e), yv.at(e) * ry, s2[0]);
       }
     });
     if constexpr (POST) red.sum(s2);
@@ -249,21 +261,21 @@ __global__ __launch_bounds__(MAXG) void norm_backward_kernel(NormBackwardArgs a)
         reach(i, c, d);
       }
       if constexpr (NEXT) {
-        const Chunk<F32> zv = z.get(i, c), gv = du.get(i, c);
+        const Chunk<F32> zv = r.z.get(i, c), gv = r.du.get(i, c);
 #pragma unroll
         for (int e = 0; e < V; ++e) o[e] = gv.at(e) * (zv.at(e) * rz);
         add(1, i, c, first, o);
       }
       if constexpr (POST) {
-        const Chunk<F32> yv = y.get(i, c), w = load_chunk<F32>(a.w, c, h);
+        const Chunk<F32> yv = r.y.get(i, c), wv = w.get(i, c);
         float dn[V];
 #pragma unroll
         for (int e = 0; e < V; ++e) {
           dn[e] = d[e];
-          g[e] = d[e] * (yv.at(e) * ry * w.at(e));
+          g[e] = d[e] * (yv.at(e) * ry * wv.at(e));
         }
         if (a.gate_mode != DEAMOE_GATE_NONE) {
-          const Chunk<F32> gv = load_chunk<F32>(gate, c, h);
+          const Chunk<F32> gv = r.gate.get(i, c);
 #pragma unroll
           for (int e = 0; e < V; ++e) dn[e] *= gv.at(e);
           if (a.gate_mode == DEAMOE_GATE_FULL)
@@ -275,7 +287,7 @@ __global__ __launch_bounds__(MAXG) void norm_backward_kernel(NormBackwardArgs a)
         for (int e = 0; e < V; ++e) o[e] = dn[e] * (yv.at(e) * ry);
         add(0, i, c, first, o);
 #pragma unroll
-        for (int e = 0; e < V; ++e) o[e] = ry * (dn[e] * w.at(e) - yv.at(e) * ry * my);
+        for (int e = 0; e < V; ++e) o[e] = ry * (dn[e] * wv.at(e) - yv.at(e) * ry * my);
         store_chunk<F32>(row_at<F32>(a.dy, t, h), c, h, pack_chunk<F32>(o));
       }
 #pragma unroll
@@ -297,25 +309,39 @@ __global__ __launch_bounds__(MAXG) void norm_backward_kernel(NormBackwardArgs a)
     });
 }
 
-// out[which][c] = sum over the workgroups' parts, four interleaved sums joined.
+// out[c] = sum over the workgroups' parts.  A workgroup takes 64 columns; its 16
+// waves take every 16th part, eight loads in flight, and are joined in order.
 struct ColumnSumArgs {
-  const float *part;
+  const float *part[3];     // stride of the parts: 3 * h
   float *out[3];
   int32_t h, blocks;
 };
-__global__ __launch_bounds__(256) void column_sum_kernel(ColumnSumArgs a) {
-  __shared__ float s_sum[4][kWave];
-  const int which = blockIdx.y;
-  if (!a.out[which]) return;
+__global__ __launch_bounds__(1024) void column_sum_kernel(ColumnSumArgs a) {
+  constexpr int W = 16, U = 8;
+  __shared__ float s_sum[W][kWave];
   const int lane = threadIdx.x % kWave, wv = threadIdx.x / kWave;
   const int c = blockIdx.x * kWave + lane;
+  const float *p = a.part[blockIdx.y] + min(c, a.h - 1);
   float v = 0.f;
-  if (c < a.h)
-    for (int b = wv; b < a.blocks; b += 4) v += a.part[((size_t)b * 3 + which) * a.h + c];
+  for (int b0 = wv; b0 < a.blocks; b0 += W * U) {
+    float t[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int b = b0 + u * W;
+      t[u] = p[(size_t)min(b, a.blocks - 1) * 3 * a.h];
+      t[u] = b < a.blocks ? t[u] : 0.f;
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) v += t[u];
+  }
   s_sum[wv][lane] = v;
   __syncthreads();
-  if (wv == 0 && c < a.h)
-    a.out[which][c] = (s_sum[0][lane] + s_sum[1][lane]) + (s_sum[2][lane] + s_sum[3][lane]);
+  if (wv == 0 && c < a.h) {
+    float total = 0.f;
+#pragma unroll
+    for (int i = 0; i < W; ++i) total += s_sum[i][lane];
+    a.out[blockIdx.y][c] = total;
+  }
 }
 
 namespace {
@@ -367,7 +393,15 @@ hipError_t with_shape(Shape sh, bool f32, F f) {
 
 }  // namespace
 
-int norm_backward_blocks(int T, int) { return T < 512 ? T : 512; }
+// As many workgroups as run at once (eight waves on each of the 256 CUs, one
+// workgroup at least), and of those as many as share the rows evenly.
+int norm_backward_blocks(int T, int h) {
+  const int threads = shape_of(h, 0).threads;   // the smaller of the two types' shapes
+  const int most = threads >= 512 ? 256 : 131072 / threads;
+  if (T <= most) return T;
+  const int rows = (T + most - 1) / most;
+  return (T + rows - 1) / rows;
+}
 
 hipError_t launch_prenorm(const PrenormArgs &a, hipStream_t s) {
   const Shape sh = shape_of(a.h, a.act_f32);
@@ -395,13 +429,17 @@ hipError_t launch_norm_backward(const NormBackwardArgs &a, hipStream_t s) {
   });
   if (e != hipSuccess) return e;
   ColumnSumArgs c;
-  c.part = a.part;
-  c.out[0] = a.y ? a.dw : nullptr;
-  c.out[1] = a.dw_next;
-  c.out[2] = a.gate_mode == DEAMOE_GATE_SHARED ? static_cast<float *>(a.dgate) : nullptr;
+  int n = 0;
+  auto sum_of = [&](int which, void *out) {
+    c.part[n] = a.part + (size_t)which * a.h;
+    c.out[n++] = static_cast<float *>(out);
+  };
+  if (a.y) sum_of(0, a.dw);
+  if (a.dw_next) sum_of(1, a.dw_next);
+  if (a.gate_mode == DEAMOE_GATE_SHARED) sum_of(2, a.dgate);
   c.h = a.h;
   c.blocks = blocks;
-  hipLaunchKernelGGL(column_sum_kernel, dim3((a.h + kWave - 1) / kWave, 3), dim3(256), 0, s, c);
+  hipLaunchKernelGGL(column_sum_kernel, dim3((a.h + kWave - 1) / kWave, n), dim3(1024), 0, s, c);
   return hipGetLastError();
 }
 
