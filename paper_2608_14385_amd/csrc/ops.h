@@ -97,9 +97,12 @@ struct DispatchArgs {
   void *xs;                 // NULL: lists only
   int32_t *hist, *total;    // workspace of a large sort
 };
-constexpr int kSortChunk = 2048;        // pairs of one workgroup of a large sort
 constexpr int kSortSmallPairs = 4096;   // up to here one launch sorts and gathers
-inline int sort_chunks(int64_t pairs) { return (int)((pairs + kSortChunk - 1) / kSortChunk); }
+// Pairs that one workgroup of a large sort counts and ranks: few, so that many
+// workgroups share the work, until their counts per group would outgrow the
+// caches.
+constexpr int kSortChunk = 512, kSortChunkLarge = 4096;
+inline int sort_chunk(int64_t pairs) { return pairs <= 1 << 18 ? kSortChunk : kSortChunkLarge; }
 hipError_t launch_dispatch(const DispatchArgs &a, hipStream_t s);
 hipError_t launch_zero(void *p, size_t bytes, hipStream_t s);   // multiples of 4 bytes
 

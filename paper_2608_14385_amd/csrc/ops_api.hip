@@ -44,7 +44,7 @@ SortLayout sort_layout(int32_t T, int32_t k, int32_t n) {
   SortLayout L{0, 0, 0};
   const int64_t P = (int64_t)T * k;
   if (P <= kSortSmallPairs) return L;
-  L.total = align16((size_t)n * sort_chunks(P) * 4);
+  L.total = align16((size_t)n * ((P + sort_chunk(P) - 1) / sort_chunk(P)) * 4);
   L.bytes = L.total + align16((size_t)n * 4);
   return L;
 }

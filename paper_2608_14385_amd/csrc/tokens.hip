@@ -4,6 +4,8 @@
 //   row_p = #{q : key_q < key_p} + #{q < p : key_q = key_p}
 // Counts are sums of integers and ranks follow the pair order, so the lists do
 // not depend on the order in which workgroups run.
+#include <type_traits>
+
 #include "ops.h"
 
 namespace deamoe {
@@ -132,12 +134,13 @@ __global__ __launch_bounds__(kThreads) void dispatch_small_kernel(DispatchArgs a
 }
 
 // Large sorts: counts per (group, chunk of pairs) ...
+template <int CHUNK>
 __global__ __launch_bounds__(kThreads) void sort_count_kernel(DispatchArgs a, int chunks) {
   __shared__ int s_count[DEAMOE_MAX_EXPERTS];
   const int P = a.T * a.k;
   for (int e = threadIdx.x; e < a.n; e += kThreads) s_count[e] = 0;
   __syncthreads();
-  const int lo = blockIdx.x * kSortChunk, hi = min(lo + kSortChunk, P);
+  const int lo = blockIdx.x * CHUNK, hi = min(lo + CHUNK, P);
   for (int p = lo + threadIdx.x; p < hi; p += kThreads) {
     const int e = key_of(a.ids[p], a.n);
     if (e < a.n) atomicAdd(&s_count[e], 1);
@@ -166,6 +169,7 @@ __global__ __launch_bounds__(kThreads) void sort_scan_kernel(DispatchArgs a, int
 // ... from which every chunk ranks its pairs.  Each wave takes a quarter of the
 // chunk, 64 pairs at a time: the lanes of one group find each other by one
 // ballot per bit of the group number.
+template <int CHUNK>
 __global__ __launch_bounds__(kThreads) void sort_rank_kernel(DispatchArgs a, int chunks) {
   __shared__ int s_offset[DEAMOE_MAX_EXPERTS];
   __shared__ int s_next[kWaves][DEAMOE_MAX_EXPERTS];   // next row of a group, per wave
@@ -183,8 +187,8 @@ __global__ __launch_bounds__(kThreads) void sort_rank_kernel(DispatchArgs a, int
     for (int e = tid; e < n; e += kThreads) a.offset[e] = s_offset[e];
     if (tid == 0) a.offset[n] = used;
   }
-  constexpr int kPart = kSortChunk / kWaves, kRounds = kPart / kWave;
-  const int lo = blockIdx.x * kSortChunk + wv * kPart;
+  constexpr int kPart = CHUNK / kWaves, kRounds = kPart / kWave;
+  const int lo = blockIdx.x * CHUNK + wv * kPart;
   int key[kRounds];
 #pragma unroll
   for (int i = 0; i < kRounds; ++i) {
@@ -247,10 +251,15 @@ hipError_t dispatch_typed(const DispatchArgs &a, hipStream_t s) {
     hipLaunchKernelGGL(dispatch_small_kernel<F32>, dim3(a.T + 1, parts), dim3(kThreads), 0, s, a);
     return hipGetLastError();
   }
-  const int chunks = sort_chunks(P);
-  hipLaunchKernelGGL(sort_count_kernel, dim3(chunks), dim3(kThreads), 0, s, a, chunks);
-  hipLaunchKernelGGL(sort_scan_kernel, dim3(a.n), dim3(kThreads), 0, s, a, chunks);
-  hipLaunchKernelGGL(sort_rank_kernel, dim3(chunks), dim3(kThreads), 0, s, a, chunks);
+  const int chunk = sort_chunk(P), chunks = (int)((P + chunk - 1) / chunk);
+  auto sort = [&](auto C) {
+    constexpr int CHUNK = decltype(C)::value;
+    hipLaunchKernelGGL(sort_count_kernel<CHUNK>, dim3(chunks), dim3(kThreads), 0, s, a, chunks);
+    hipLaunchKernelGGL(sort_scan_kernel, dim3(a.n), dim3(kThreads), 0, s, a, chunks);
+    hipLaunchKernelGGL(sort_rank_kernel<CHUNK>, dim3(chunks), dim3(kThreads), 0, s, a, chunks);
+  };
+  if (chunk == kSortChunk) sort(std::integral_constant<int, kSortChunk>{});
+  else sort(std::integral_constant<int, kSortChunkLarge>{});
   if (a.xs)
     hipLaunchKernelGGL(gather_rows_kernel<F32>, dim3(a.T, parts), dim3(kThreads), 0, s, a);
   return hipGetLastError();

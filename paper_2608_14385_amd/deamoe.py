@@ -7,6 +7,7 @@ fallback path.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes as C
 import os
 from dataclasses import dataclass
@@ -290,14 +291,13 @@ class Layer:
 # workspace is given, take one from torch's allocator for that stream.
 
 
-def _fits(what: str, dev, **tensors):
-    """Every (tensor, dtype, shape) has that type and shape, is contiguous and on `dev`."""
-    for name, (t, dtype, shape) in tensors.items():
-        if t.dtype is not dtype or t.shape != shape:
-            raise DeamoeError(ERR_INVALID, f"{what}: {name} is {t.dtype} {tuple(t.shape)}, "
-                                           f"needed is {dtype} {tuple(shape)}")
-        if not t.is_contiguous() or t.device != dev:
-            raise DeamoeError(ERR_INVALID, f"{what}: {name} is not contiguous, or not on {dev}")
+def _fits(what: str, dev: int, *tensors):
+    """Every (name, tensor, dtype, shape) has that type and shape, is contiguous and on device `dev`."""
+    for name, t, dtype, shape in tensors:
+        if t.dtype is not dtype or t.shape != shape or t.get_device() != dev or not t.is_contiguous():
+            raise DeamoeError(ERR_INVALID, f"{what}: {name} is {t.dtype} {tuple(t.shape)} with strides "
+                              f"{t.stride()} on {t.device}; needed is {dtype} {tuple(shape)}, contiguous, "
+                              f"on device {dev}")
 
 
 def _act(what: str, t: torch.Tensor) -> int:
@@ -308,29 +308,31 @@ def _act(what: str, t: torch.Tensor) -> int:
     raise DeamoeError(ERR_INVALID, f"{what}: {t.dtype} is neither bfloat16 nor float32")
 
 
-def _run(fn, dev, stream, *args):
-    """fn(*args, stream) with the tensors' device current."""
-    if dev.type != "cuda":
-        raise DeamoeError(ERR_INVALID, f"{fn.__name__}: tensors are on {dev}, not on a GPU")
-    if dev.index == torch.cuda.current_device():
-        status = fn(*args, _stream(stream))
-    else:
+def _call(fn, dev: int, stream, args) -> int:
+    """fn(*args, stream) with device `dev` current; the stream is its current one unless given."""
+    if dev < 0:
+        raise DeamoeError(ERR_INVALID, f"{fn.__name__}: tensors are not on a GPU")
+    if dev != torch.cuda.current_device():
         with torch.cuda.device(dev):
-            status = fn(*args, _stream(stream))
+            return _call(fn, dev, stream, args)
+    return fn(*args, torch.cuda.current_stream().cuda_stream if stream is None else stream.cuda_stream)
+
+
+def _run(fn, dev: int, stream, *args):
+    _check(_call(fn, dev, stream, args), fn.__name__)
+
+
+def _run_with_workspace(fn, dev: int, stream, ws, nbytes, *args):
+    """The same for a call that may need a workspace of nbytes() (its last two arguments): the given
+    one, or one of torch's for the stream that the call runs on, asked for if the call wants it."""
+    if ws is not None and (ws.get_device() != dev or not ws.is_contiguous()):
+        raise DeamoeError(ERR_WORKSPACE, f"{fn.__name__}: workspace is not contiguous, or not on device {dev}")
+    status = _call(fn, dev, stream, (*args, _ptr(ws), 0 if ws is None else ws.numel() * ws.element_size()))
+    if status == ERR_WORKSPACE and ws is None:
+        with contextlib.nullcontext() if stream is None else torch.cuda.stream(stream):
+            ws = torch.empty(nbytes(), dtype=torch.uint8, device=f"cuda:{dev}")
+        status = _call(fn, dev, stream, (*args, ws.data_ptr(), ws.numel()))
     _check(status, fn.__name__)
-
-
-def _workspace(ws, dev, stream, nbytes: int):
-    """(pointer, size) and the tensor that keeps it: `ws`, or one of torch's for `stream`."""
-    if ws is None and nbytes and dev.type == "cuda":
-        if stream is None:
-            ws = torch.empty(nbytes, dtype=torch.uint8, device=dev)
-        else:
-            with torch.cuda.stream(stream):
-                ws = torch.empty(nbytes, dtype=torch.uint8, device=dev)
-    elif ws is not None and (ws.device != dev or not ws.is_contiguous()):
-        raise DeamoeError(ERR_WORKSPACE, f"workspace is not contiguous, or not on {dev}")
-    return (None, 0, None) if ws is None else (ws.data_ptr(), ws.numel() * ws.element_size(), ws)
 
 
 def _bytes(fn, *args) -> int:
@@ -354,25 +356,25 @@ def deamoe_dispatch(ids, x, offset, pair, row, xs=None, ws=None, stream=None):
     with xs [T * k, h] the rows of x [T, h] in that order (x may be None without xs)."""
     what, i32 = "deamoe_dispatch", torch.int32
     T, k = _rows(what, ids, "ids")
-    dev, n, h, act = ids.device, offset.numel() - 1, 1, F32
-    _fits(what, dev, ids=(ids, i32, ids.shape), offset=(offset, i32, (n + 1,)),
-          pair=(pair, i32, (T * k,)), row=(row, i32, (T, k)))
+    dev, n, h, act = ids.get_device(), offset.numel() - 1, 1, F32
+    _fits(what, dev, ("ids", ids, i32, (T, k)), ("offset", offset, i32, (n + 1,)),
+          ("pair", pair, i32, (T * k,)), ("row", row, i32, (T, k)))
     if xs is not None:
         act, h = _act(what, x), _rows(what, x, "x")[1]
-        _fits(what, dev, x=(x, x.dtype, (T, h)), xs=(xs, x.dtype, (T * k, h)))
-    wp, wn, keep = _workspace(ws, dev, stream, deamoe_dispatch_workspace_bytes(T, k, n))
-    _run(lib().deamoe_dispatch, dev, stream, T, k, n, h, act, ids.data_ptr(),
-         _ptr(x) if xs is not None else None, offset.data_ptr(), pair.data_ptr(), row.data_ptr(),
-         _ptr(xs), wp, wn)
+        _fits(what, dev, ("x", x, x.dtype, (T, h)), ("xs", xs, x.dtype, (T * k, h)))
+    _run_with_workspace(lib().deamoe_dispatch, dev, stream, ws,
+                        lambda: deamoe_dispatch_workspace_bytes(T, k, n), T, k, n, h, act,
+                        ids.data_ptr(), x.data_ptr() if xs is not None else None, offset.data_ptr(),
+                        pair.data_ptr(), row.data_ptr(), _ptr(xs))
 
 
 def deamoe_dispatch_backward(row, dxs, dx, stream=None):
     """dx [T, h]: the sum of each token's rows of dxs [T * k, h]."""
     what = "deamoe_dispatch_backward"
-    (T, k), h, dev = _rows(what, row, "row"), _rows(what, dx, "dx")[1], row.device
+    (T, k), h, dev, dt = _rows(what, row, "row"), _rows(what, dx, "dx")[1], row.get_device(), dx.dtype
     act = _act(what, dx)
-    _fits(what, dev, row=(row, torch.int32, (T, k)), dx=(dx, dx.dtype, (T, h)),
-          dxs=(dxs, dx.dtype, (T * k, h)))
+    _fits(what, dev, ("row", row, torch.int32, (T, k)), ("dx", dx, dt, (T, h)),
+          ("dxs", dxs, dt, (T * k, h)))
     _run(lib().deamoe_dispatch_backward, dev, stream, T, k, h, act, row.data_ptr(),
          dxs.data_ptr(), dx.data_ptr())
 
@@ -380,10 +382,10 @@ def deamoe_dispatch_backward(row, dxs, dx, stream=None):
 def deamoe_combine(row, w, ys, y, stream=None):
     """y [T, h]: the sum of each token's rows of ys [T * k, h], weighted by w [T, k] (fp32)."""
     what = "deamoe_combine"
-    (T, k), h, dev = _rows(what, row, "row"), _rows(what, y, "y")[1], row.device
+    (T, k), h, dev, dt = _rows(what, row, "row"), _rows(what, y, "y")[1], row.get_device(), y.dtype
     act = _act(what, y)
-    _fits(what, dev, row=(row, torch.int32, (T, k)), w=(w, torch.float32, (T, k)),
-          y=(y, y.dtype, (T, h)), ys=(ys, y.dtype, (T * k, h)))
+    _fits(what, dev, ("row", row, torch.int32, (T, k)), ("w", w, torch.float32, (T, k)),
+          ("y", y, dt, (T, h)), ("ys", ys, dt, (T * k, h)))
     _run(lib().deamoe_combine, dev, stream, T, k, h, act, row.data_ptr(), w.data_ptr(),
          ys.data_ptr(), y.data_ptr())
 
@@ -391,38 +393,36 @@ def deamoe_combine(row, w, ys, y, stream=None):
 def deamoe_combine_backward(row, w, ys, dy, dys=None, dw=None, stream=None):
     """dys [T * k, h] and dw [T, k] (either may be None) from dy [T, h]; w is needed for dys only,
     ys for dw only."""
-    what = "deamoe_combine_backward"
-    (T, k), h, dev = _rows(what, row, "row"), _rows(what, dy, "dy")[1], row.device
-    act, f32 = _act(what, dy), torch.float32
-    _fits(what, dev, row=(row, torch.int32, (T, k)), dy=(dy, dy.dtype, (T, h)),
-          **({"dys": (dys, dy.dtype, (T * k, h)), "w": (w, f32, (T, k))} if dys is not None else {}),
-          **({"dw": (dw, f32, (T, k)), "ys": (ys, dy.dtype, (T * k, h))} if dw is not None else {}))
+    what, f32 = "deamoe_combine_backward", torch.float32
+    (T, k), h, dev, dt = _rows(what, row, "row"), _rows(what, dy, "dy")[1], row.get_device(), dy.dtype
+    act = _act(what, dy)
+    _fits(what, dev, ("row", row, torch.int32, (T, k)), ("dy", dy, dt, (T, h)))
+    if dys is not None:
+        _fits(what, dev, ("dys", dys, dt, (T * k, h)), ("w", w, f32, (T, k)))
+    if dw is not None:
+        _fits(what, dev, ("dw", dw, f32, (T, k)), ("ys", ys, dt, (T * k, h)))
     _run(lib().deamoe_combine_backward, dev, stream, T, k, h, act, row.data_ptr(),
-         _ptr(w) if dys is not None else None, _ptr(ys) if dw is not None else None, dy.data_ptr(),
-         _ptr(dys), _ptr(dw))
+         w.data_ptr() if dys is not None else None, ys.data_ptr() if dw is not None else None,
+         dy.data_ptr(), _ptr(dys), _ptr(dw))
 
 
 def _w4(what: str, x, matrices, y, offset):
     """Checks one product's tensors: its config, rows and device."""
     codes, scale = matrices[0]
     M, K = _rows(what, x, "x")
-    R, half = codes.shape[-2:] if codes.dim() > 1 else (0, 0)
-    if codes.dim() not in (2, 3) or half * 2 != K or scale.dim() != codes.dim() or not scale.shape[-1]:
-        raise DeamoeError(ERR_INVALID, f"{what}: codes {tuple(codes.shape)} and scale "
-                                       f"{tuple(scale.shape)} do not fit {K} columns")
-    n = codes.shape[0] if codes.dim() == 3 else 1
-    group, dev, sdt = K // scale.shape[-1], x.device, scale.dtype
-    if group * scale.shape[-1] != K or sdt not in (torch.float32, torch.bfloat16):
-        raise DeamoeError(ERR_INVALID, f"{what}: scale is {sdt} {tuple(scale.shape)} for {K} columns")
+    shape, groups = codes.shape, scale.shape[-1] if scale.dim() else 0
+    if len(shape) not in (2, 3) or shape[-1] * 2 != K or scale.dim() != len(shape) or not groups or K % groups:
+        raise DeamoeError(ERR_INVALID, f"{what}: codes {tuple(shape)} and scale {tuple(scale.shape)} "
+                                       f"do not fit {K} columns")
+    n, R, dev, sdt, bf16 = shape[0] if len(shape) == 3 else 1, shape[-2], x.get_device(), scale.dtype, torch.bfloat16
+    if sdt is not torch.float32 and sdt is not bf16:
+        raise DeamoeError(ERR_INVALID, f"{what}: scale is {sdt}")
     for c, s in matrices:
-        _fits(what, dev, codes=(c, torch.uint8, codes.shape),
-              scale=(s, sdt, (*codes.shape[:-1], K // group)))
-    _fits(what, dev, x=(x, torch.bfloat16, (M, K)), y=(y, torch.bfloat16, (M, R)))
+        _fits(what, dev, ("codes", c, torch.uint8, shape), ("scale", s, sdt, (*shape[:-1], groups)))
+    _fits(what, dev, ("x", x, bf16, (M, K)), ("y", y, bf16, (M, R)))
     if offset is not None:
-        _fits(what, dev, offset=(offset, torch.int32, (n + 1,)))
-    cfg = deamoe_w4_config(R=R, K=K, n=n, group=group,
-                           scale_dtype=BF16 if sdt is torch.bfloat16 else F32)
-    return cfg, M, dev
+        _fits(what, dev, ("offset", offset, torch.int32, (n + 1,)))
+    return deamoe_w4_config(R, K, n, K // groups, BF16 if sdt is bf16 else F32), M, dev
 
 
 def deamoe_w4_linear(x, codes, scale, y, offset=None, stream=None):
@@ -449,28 +449,31 @@ def deamoe_norm_workspace_bytes(T: int, h: int) -> int:
 def deamoe_prenorm(x, w, u, eps: float = 1e-6, stream=None):
     """u = RMSNorm(x) * w, rows of x [T, h]; u may be x."""
     what = "deamoe_prenorm"
-    (T, h), act, dev, dt = _rows(what, x, "x"), _act(what, x), x.device, x.dtype
-    _fits(what, dev, x=(x, dt, (T, h)), w=(w, dt, (h,)), u=(u, dt, (T, h)))
+    (T, h), act, dev, dt = _rows(what, x, "x"), _act(what, x), x.get_device(), x.dtype
+    _fits(what, dev, ("x", x, dt, (T, h)), ("w", w, dt, (h,)), ("u", u, dt, (T, h)))
     _run(lib().deamoe_prenorm, dev, stream, T, h, act, eps, x.data_ptr(), w.data_ptr(),
          u.data_ptr())
 
 
 def deamoe_prenorm_backward(x, w, du, dx, dw, dres=None, eps: float = 1e-6, ws=None, stream=None):
     """dx = dres + the gradient of x from du; dw [h] fp32.  dres may be dx."""
-    what, f32 = "deamoe_prenorm_backward", torch.float32
-    (T, h), act, dev, dt = _rows(what, x, "x"), _act(what, x), x.device, x.dtype
-    _fits(what, dev, x=(x, dt, (T, h)), w=(w, dt, (h,)), du=(du, dt, (T, h)), dx=(dx, dt, (T, h)),
-          dw=(dw, f32, (h,)), **({"dres": (dres, dt, (T, h))} if dres is not None else {}))
-    wp, wn, keep = _workspace(ws, dev, stream, deamoe_norm_workspace_bytes(T, h))
-    _run(lib().deamoe_prenorm_backward, dev, stream, T, h, act, eps, x.data_ptr(), w.data_ptr(),
-         du.data_ptr(), _ptr(dres), dx.data_ptr(), dw.data_ptr(), wp, wn)
+    what = "deamoe_prenorm_backward"
+    (T, h), act, dev, dt = _rows(what, x, "x"), _act(what, x), x.get_device(), x.dtype
+    _fits(what, dev, ("x", x, dt, (T, h)), ("w", w, dt, (h,)), ("du", du, dt, (T, h)),
+          ("dx", dx, dt, (T, h)), ("dw", dw, torch.float32, (h,)))
+    if dres is not None:
+        _fits(what, dev, ("dres", dres, dt, (T, h)))
+    _run_with_workspace(lib().deamoe_prenorm_backward, dev, stream, ws,
+                        lambda: deamoe_norm_workspace_bytes(T, h), T, h, act, eps, x.data_ptr(),
+                        w.data_ptr(), du.data_ptr(), _ptr(dres), dx.data_ptr(), dw.data_ptr())
 
 
 def _gate(what, gate, T, h, dt, dev) -> int:
     if gate is None:
         return GATE_NONE
-    _fits(what, dev, gate=(gate, dt, (h,) if gate.dim() == 1 else (T, h)))
-    return GATE_SHARED if gate.dim() == 1 else GATE_FULL
+    shared = gate.dim() == 1
+    _fits(what, dev, ("gate", gate, dt, (h,) if shared else (T, h)))
+    return GATE_SHARED if shared else GATE_FULL
 
 
 def deamoe_postnorm(x, y, w, z, gate=None, res_scale: float = 1.0, w_next=None, u=None,
@@ -478,10 +481,13 @@ def deamoe_postnorm(x, y, w, z, gate=None, res_scale: float = 1.0, w_next=None, 
     """z = res_scale * x + gate * RMSNorm(y) * w, rows of x and y [T, h]; gate [h], [T, h] or None (1).
     With w_next and u also u = RMSNorm(z) * w_next.  z may be x."""
     what = "deamoe_postnorm"
-    (T, h), act, dev, dt = _rows(what, x, "x"), _act(what, x), x.device, x.dtype
-    _fits(what, dev, x=(x, dt, (T, h)), y=(y, dt, (T, h)), w=(w, dt, (h,)), z=(z, dt, (T, h)),
-          **({"w_next": (w_next, dt, (h,))} if w_next is not None else {}),
-          **({"u": (u, dt, (T, h))} if u is not None else {}))
+    (T, h), act, dev, dt = _rows(what, x, "x"), _act(what, x), x.get_device(), x.dtype
+    full = (T, h)
+    _fits(what, dev, ("x", x, dt, full), ("y", y, dt, full), ("w", w, dt, (h,)), ("z", z, dt, full))
+    if w_next is not None:
+        _fits(what, dev, ("w_next", w_next, dt, (h,)))
+    if u is not None:
+        _fits(what, dev, ("u", u, dt, full))
     mode = _gate(what, gate, T, h, dt, dev)
     _run(lib().deamoe_postnorm, dev, stream, T, h, act, eps, res_scale, mode, x.data_ptr(),
          y.data_ptr(), w.data_ptr(), _ptr(gate), _ptr(w_next), z.data_ptr(), _ptr(u))
@@ -493,22 +499,22 @@ def deamoe_postnorm_backward(y, w, dz, dx, dy, dw, gate=None, dgate=None, res_sc
     """Gradients of deamoe_postnorm from dz and, with a next norm (z, w_next, du, dw_next), du: dx, dy
     [T, h], dw and dw_next [h] fp32, dgate as the gate ([h]: fp32).  dx may be dz."""
     what, f32 = "deamoe_postnorm_backward", torch.float32
-    (T, h), act, dev, dt = _rows(what, y, "y"), _act(what, y), y.device, y.dtype
+    (T, h), act, dev, dt = _rows(what, y, "y"), _act(what, y), y.get_device(), y.dtype
     mode, full, vec = _gate(what, gate, T, h, dt, dev), (T, h), (h,)
-    _fits(what, dev, y=(y, dt, full), w=(w, dt, vec), dz=(dz, dt, full), dx=(dx, dt, full),
-          dy=(dy, dt, full), dw=(dw, f32, vec))
+    _fits(what, dev, ("y", y, dt, full), ("w", w, dt, vec), ("dz", dz, dt, full), ("dx", dx, dt, full),
+          ("dy", dy, dt, full), ("dw", dw, f32, vec))
     if (dgate is None) != (mode == GATE_NONE) or len({t is None for t in (z, w_next, du, dw_next)}) != 1:
         raise DeamoeError(ERR_INVALID, f"{what}: gate and dgate, and z, w_next, du and dw_next, are "
                                        "given together or not at all")
     if dgate is not None:
-        _fits(what, dev, dgate=(dgate, f32, vec) if mode == GATE_SHARED else (dgate, dt, full))
+        _fits(what, dev, ("dgate", dgate, f32, vec) if mode == GATE_SHARED else ("dgate", dgate, dt, full))
     if du is not None:
-        _fits(what, dev, z=(z, dt, full), w_next=(w_next, dt, vec), du=(du, dt, full),
-              dw_next=(dw_next, f32, vec))
-    wp, wn, keep = _workspace(ws, dev, stream, deamoe_norm_workspace_bytes(T, h))
-    _run(lib().deamoe_postnorm_backward, dev, stream, T, h, act, eps, res_scale, mode, y.data_ptr(),
-         w.data_ptr(), _ptr(gate), _ptr(z), _ptr(w_next), dz.data_ptr(), _ptr(du), dx.data_ptr(),
-         dy.data_ptr(), dw.data_ptr(), _ptr(dgate), _ptr(dw_next), wp, wn)
+        _fits(what, dev, ("z", z, dt, full), ("w_next", w_next, dt, vec), ("du", du, dt, full),
+              ("dw_next", dw_next, f32, vec))
+    _run_with_workspace(lib().deamoe_postnorm_backward, dev, stream, ws,
+                        lambda: deamoe_norm_workspace_bytes(T, h), T, h, act, eps, res_scale, mode,
+                        y.data_ptr(), w.data_ptr(), _ptr(gate), _ptr(z), _ptr(w_next), dz.data_ptr(),
+                        _ptr(du), dx.data_ptr(), dy.data_ptr(), dw.data_ptr(), _ptr(dgate), _ptr(dw_next))
 
 
 class W4Experts:
