@@ -13,9 +13,14 @@ namespace deamoe {
 template <bool F32>
 inline constexpr int kVec = F32 ? 4 : 8;
 
-struct __attribute__((packed, aligned(2))) Raw16 {
-  u32x4 v;
-};
+typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
+
+// STREAM: an access that keeps its lines out of the caches' way.  Loads of rows
+// that are read once (8192 x 8 rows of 4096, 539 MB, collected in 101 us, not
+// 119; 1024 x 8 in 13 us, not 19), and stores of more than the 256 MB of the
+// last-level cache can keep for the next kernel (the same 539 MB dispatched in
+// 94 us, not 113; of 67 MB no faster).
+constexpr int64_t kStreamBytes = 256 << 20;
 
 template <bool F32>
 struct Chunk {
@@ -27,13 +32,14 @@ struct Chunk {
 };
 
 // Elements [c, c + kVec) of the row at p (h elements); zeros past the end.
-template <bool F32>
+template <bool F32, bool STREAM = false>
 __device__ inline Chunk<F32> load_chunk(const void *p, int c, int h) {
   constexpr int V = kVec<F32>;
   Chunk<F32> r;
   const char *q = static_cast<const char *>(p) + (size_t)c * (F32 ? 4 : 2);
   if (c + V <= h) {
-    r.raw = reinterpret_cast<const Raw16 *>(q)->v;
+    const auto *v = reinterpret_cast<const u32x4_any *>(q);
+    r.raw = STREAM ? __builtin_nontemporal_load(v) : *v;
   } else {
     r.raw = u32x4{0, 0, 0, 0};
 #pragma unroll
@@ -46,12 +52,14 @@ __device__ inline Chunk<F32> load_chunk(const void *p, int c, int h) {
   return r;
 }
 
-template <bool F32>
+template <bool F32, bool STREAM = false>
 __device__ inline void store_chunk(void *p, int c, int h, const Chunk<F32> &r) {
   constexpr int V = kVec<F32>;
   char *q = static_cast<char *>(p) + (size_t)c * (F32 ? 4 : 2);
   if (c + V <= h) {
-    reinterpret_cast<Raw16 *>(q)->v = r.raw;
+    auto *v = reinterpret_cast<u32x4_any *>(q);
+    if constexpr (STREAM) __builtin_nontemporal_store((u32x4_any)r.raw, v);
+    else *v = r.raw;
   } else {
 #pragma unroll
     for (int i = 0; i < V; ++i)

@@ -55,12 +55,12 @@ __device__ inline int scan_counts(int *counts, int n, int *s_wave) {
 }
 
 // Chunks of x of one token stored to its rows.
-template <bool F32>
+template <bool F32, bool STREAM = false>
 __device__ inline void scatter_row(const DispatchArgs &a, const int *rows, int c,
                                    const Chunk<F32> &v) {
   for (int s = 0; s < a.k; ++s) {
     const int r = rows[s];
-    if (r >= 0) store_chunk<F32>(row_at<F32>(a.xs, r, a.h), c, a.h, v);
+    if (r >= 0) store_chunk<F32, STREAM>(row_at<F32>(a.xs, r, a.h), c, a.h, v);
   }
 }
 
@@ -233,11 +233,11 @@ __global__ __launch_bounds__(kThreads) void sort_rank_kernel(DispatchArgs a, int
 }
 
 // Every token's row read once and stored to its k rows.
-template <bool F32>
+template <bool F32, bool STREAM>
 __global__ __launch_bounds__(kThreads) void gather_rows_kernel(DispatchArgs a) {
   const int t = blockIdx.x, c = (blockIdx.y * kThreads + threadIdx.x) * kVec<F32>;
   if (c >= a.h) return;
-  scatter_row<F32>(a, a.row + (size_t)t * a.k, c,
+  scatter_row<F32, STREAM>(a, a.row + (size_t)t * a.k, c,
                    load_chunk<F32>(row_at<F32>(a.x, t, a.h), c, a.h));
 }
 
@@ -260,8 +260,10 @@ hipError_t dispatch_typed(const DispatchArgs &a, hipStream_t s) {
   };
   if (chunk == kSortChunk) sort(std::integral_constant<int, kSortChunk>{});
   else sort(std::integral_constant<int, kSortChunkLarge>{});
-  if (a.xs)
-    hipLaunchKernelGGL(gather_rows_kernel<F32>, dim3(a.T, parts), dim3(kThreads), 0, s, a);
+  if (a.xs && P * a.h * (F32 ? 4 : 2) > kStreamBytes)
+    hipLaunchKernelGGL((gather_rows_kernel<F32, true>), dim3(a.T, parts), dim3(kThreads), 0, s, a);
+  else if (a.xs)
+    hipLaunchKernelGGL((gather_rows_kernel<F32, false>), dim3(a.T, parts), dim3(kThreads), 0, s, a);
   return hipGetLastError();
 }
 
@@ -303,7 +305,7 @@ __global__ __launch_bounds__(kThreads) void collect_kernel(CollectArgs a) {
       v[u].raw = u32x4{0, 0, 0, 0};
       f[u] = 0.f;
       if ((uint32_t)r < (uint32_t)rows) {
-        v[u] = load_chunk<F32>(row_at<F32>(a.ys, r, a.h), c, a.h);
+        v[u] = load_chunk<F32, true>(row_at<F32>(a.ys, r, a.h), c, a.h);
         f[u] = w ? w[s0 + u] : 1.f;
       }
     }
@@ -326,7 +328,7 @@ hipError_t launch_collect(const CollectArgs &a, hipStream_t s) {
 // dys[row] = w * dy[t] and dw = <dy[t], ys[row]>: one workgroup per token, a
 // batch of slots at a time; each thread's products of a slot are summed over
 // its columns, then over the wave, then over the waves.
-template <bool F32>
+template <bool F32, bool STREAM>
 __global__ __launch_bounds__(kThreads) void collect_backward_kernel(CollectBackwardArgs a) {
   constexpr int U = 4, V = kVec<F32>;
   __shared__ float s_dot[DEAMOE_MAX_TOPK][kWaves];
@@ -350,7 +352,7 @@ __global__ __launch_bounds__(kThreads) void collect_backward_kernel(CollectBackw
 #pragma unroll
         for (int u = 0; u < U; ++u) {
           v[u].raw = u32x4{0, 0, 0, 0};
-          if (r[u] >= 0) v[u] = load_chunk<F32>(row_at<F32>(a.ys, r[u], a.h), c, a.h);
+          if (r[u] >= 0) v[u] = load_chunk<F32, true>(row_at<F32>(a.ys, r[u], a.h), c, a.h);
         }
 #pragma unroll
       for (int u = 0; u < U; ++u) {
@@ -362,7 +364,7 @@ __global__ __launch_bounds__(kThreads) void collect_backward_kernel(CollectBackw
           float g[V];
 #pragma unroll
           for (int i = 0; i < V; ++i) g[i] = f[u] * d.at(i);
-          store_chunk<F32>(row_at<F32>(a.dys, r[u], a.h), c, a.h, pack_chunk<F32>(g));
+          store_chunk<F32, STREAM>(row_at<F32>(a.dys, r[u], a.h), c, a.h, pack_chunk<F32>(g));
         }
       }
     }
@@ -385,10 +387,10 @@ __global__ __launch_bounds__(kThreads) void collect_backward_kernel(CollectBackw
 }
 
 hipError_t launch_collect_backward(const CollectBackwardArgs &a, hipStream_t s) {
-  if (a.act_f32)
-    hipLaunchKernelGGL(collect_backward_kernel<true>, dim3(a.T), dim3(kThreads), 0, s, a);
-  else
-    hipLaunchKernelGGL(collect_backward_kernel<false>, dim3(a.T), dim3(kThreads), 0, s, a);
+  const bool stream = (int64_t)a.T * a.k * a.h * (a.act_f32 ? 4 : 2) > kStreamBytes;
+  auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(a.T), dim3(kThreads), 0, s, a); };
+  if (a.act_f32) launch(stream ? collect_backward_kernel<true, true> : collect_backward_kernel<true, false>);
+  else launch(stream ? collect_backward_kernel<false, true> : collect_backward_kernel<false, false>);
   return hipGetLastError();
 }
 
