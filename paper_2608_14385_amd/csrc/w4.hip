@@ -114,6 +114,14 @@ struct Tiles {
   }
 };
 
+// f(pointer) with the scales' type: one branch around a batch of loads, which
+// are all in flight before the first is waited for.
+template <class F>
+__device__ inline void with_scales(const void *p, int bf16, F f) {
+  if (bf16) f(glob(static_cast<const uint16_t *>(p)), 16);
+  else f(glob(static_cast<const uint32_t *>(p)), 0);
+}
+
 // A pointer every lane holds alike, in scalar registers.
 template <class P>
 __device__ inline P *uniform_ptr(P *p) {
@@ -179,9 +187,10 @@ __device__ inline void rows_together(u32x4 &a, u32x4 &b) {
 
 }  // namespace
 
-// Few token rows: the weights are streamed, each byte once per 16 * NTT rows.
-// A wave takes NR 16-row tiles of each matrix and every ks-th step of 128 * CH
-// columns.  The loads of a step are requested D steps ahead, straight into
+// Few token rows: the weights are streamed, each byte once per 16 * NTT rows
+// (KEEP: through the caches, for another 16 rows to come).  A wave takes NR
+// 16-row tiles of each matrix and every ks-th step of 256 columns.  The loads of
+// a step are requested two steps ahead, straight into
 // registers, each load 8 whole cache lines (halves of 16 lines streamed at 4.8
 // TB/s, these at 5.6, by loads alone on 490 MB).  The token rows
 // stand in LDS, a panel of columns at a time, already in the codes' order: read
@@ -194,15 +203,16 @@ __device__ inline void rows_together(u32x4 &a, u32x4 &b) {
 constexpr int kPanelWords = 16 * (1024 + 8) / 2;   // of a token tile, 4 bytes each
 constexpr int kPanelScales = 32;                   // of a weight row, at most
 constexpr int kNonTemporal = 2;                    // cache policy of a buffer load
-template <int MATS, int NR, int NTT, int G32, bool SBF, int D, int CH>
+constexpr int kRingColumns = 512;                  // two steps of 256: a round of the ring
+template <int MATS, int NR, int NTT, int G32, bool KEEP>
 __global__ __launch_bounds__(kThreads, 2) void w4_stream_kernel(W4Args a, int ks) {
-  constexpr int SC = 128 * CH, NT = MATS * NR, GS = 32 * G32;
+  constexpr int D = 2, CH = 2, SC = 128 * CH, NT = MATS * NR, GS = 32 * G32;
   constexpr int TR = NTT * kTile, WORDS = kPanelWords * NTT;
   __shared__ __align__(16) uint32_t s_x[WORDS];
   __shared__ float s_scale[kWaves][NT][kTile][kPanelScales + 1];
   static_assert(kWaves * NT * NTT * 4 * kWave <= WORDS, "the sums of the waves");
   static_assert(CH % 2 == 0, "steps of whole cache lines");
-  static_assert(D * CH * 128 <= 1024, "a panel holds a round of the ring at 16 * NTT rows");
+  static_assert(D * SC == kRingColumns && kRingColumns <= 1024, "a panel holds a round of the ring");
   const int lane = lane_id(), j = lane & 15, g = lane >> 4, tid = threadIdx.x;
   const int wv = uniform(tid / kWave);
   const int kp = wv % ks, rows = kWaves / ks * NR * kTile, rt = (a.R + rows - 1) / rows;
@@ -229,7 +239,7 @@ __global__ __launch_bounds__(kThreads, 2) void w4_stream_kernel(W4Args a, int ks
 #pragma unroll
     for (int n = 0; n < MATS; ++n) {
       wb[n] = const_cast<char *>(uniform_ptr(static_cast<const char *>(a.w[n]) + first * wrow));
-      sb[n] = uniform_ptr(static_cast<const char *>(a.scale[n]) + first * groups * (SBF ? 2 : 4));
+      sb[n] = uniform_ptr(static_cast<const char *>(a.scale[n]) + first * groups * (a.scale_bf16 ? 2 : 4));
     }
     uint32_t wo[NR][2];   // rows_together's order
 #pragma unroll
@@ -246,7 +256,7 @@ __global__ __launch_bounds__(kThreads, 2) void w4_stream_kernel(W4Args a, int ks
 #pragma unroll
         for (int c = 0; c < CH; ++c)
           W[q][n][c] =
-              __builtin_amdgcn_raw_buffer_load_b128(buf, wo[n % NR][c & 1] + c / 2 * 128, at, kNonTemporal);
+              __builtin_amdgcn_raw_buffer_load_b128(buf, wo[n % NR][c & 1] + c / 2 * 128, at, KEEP ? 0 : kNonTemporal);
       }
     };
 #pragma unroll
@@ -305,43 +315,51 @@ __global__ __launch_bounds__(kThreads, 2) void w4_stream_kernel(W4Args a, int ks
     for (int p0 = 0; p0 < a.K; p0 += pcol) {
       __syncthreads();   // the last panel, or the last item's sums, have been read
       const int q0 = p0 / GS, nq = min(groups - q0, pcol / GS);
-      float sv[NT][kTile * kPanelScales / kWave];
+      // this wave's scales, two rows at a time; past the end the sums are 0, and
+      // their scale is
+      constexpr int N = kTile * kPanelScales / kWave;
+      const int sr = lane / kPanelScales, sq = lane % kPanelScales;
+      uint32_t sv[NT][N];
 #pragma unroll
       for (int n = 0; n < NT; ++n)
+        with_scales(sb[n / NR], a.scale_bf16, [&](auto *from, int) {
 #pragma unroll
-        for (int i = 0; i < kTile * kPanelScales / kWave; ++i) {   // two rows at a time
-          const int r = (n % NR) * kTile + i * 2 + lane / kPanelScales, q = lane % kPanelScales;
-          // past the end the sums are 0, and their scale is
-          const bool ok = q < nq && r < left;
-          const uint32_t at = ok ? r * groups + q0 + q : 0;
-          float v;
-          if constexpr (SBF) v = bf16_to_f32(glob(static_cast<const uint16_t *>(sb[n / NR]))[at]);
-          else v = glob(static_cast<const float *>(sb[n / NR]))[at];
-          sv[n][i] = ok ? v : 0.f;
-        }
-      constexpr int U = 4;   // 16-byte chunks of x in flight
+          for (int i = 0; i < N; ++i) {
+            const int r = (n % NR) * kTile + i * 2 + sr;
+            sv[n][i] = from[sq < nq && r < left ? r * groups + q0 + sq : 0];
+          }
+        });
+      constexpr int U = NTT == 1 ? 8 : 16;   // 16-byte chunks of x in flight
       const int chunks = pcol / 8, total = prow * chunks;
-      for (int i0 = tid; i0 < total; i0 += U * kThreads) {
+      // i / chunks = i * inverse / 2^32: both are below 2^15, so that the
+      // inverse's excess times i stays below 2^32
+      const uint32_t inverse = 0xffffffffu / chunks + 1;
+      for (int i0 = 0; i0 < total; i0 += U * kThreads) {
         u32x4 v[U];
-        int at[U];
+        uint32_t at[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-          const int i = i0 + u * kThreads, r = i / chunks, k = (i - r * chunks) * 8;
-          const bool ok = i < total && p0 + k < a.K;
-          at[u] = i < total ? (r * ldx + k) * 2 : -1;
-          v[u] = *gptr(static_cast<const char *>(a.x) + (ok ? ((size_t)(m0 + r) * a.K + p0 + k) * 2 : 0));
-          if (!ok) v[u] = u32x4{0, 0, 0, 0};
+          if (i0 + u * kThreads >= total) break;
+          const uint32_t i = min(i0 + u * kThreads + tid, total - 1), r = __umulhi(i, inverse);
+          const uint32_t k = (i - r * chunks) * 8;
+          const bool ok = p0 + k < (uint32_t)a.K;
+          at[u] = (r * ldx + k) * 2 + !ok;   // odd: zeros, once all loads are on their way
+          v[u] = *gptr(static_cast<const char *>(a.x) + ((size_t)(m0 + r) * a.K + (ok ? p0 + k : 0)) * 2);
         }
 #pragma unroll
-        for (int u = 0; u < U; ++u)
-          if (at[u] >= 0)
-            *reinterpret_cast<bf16x8 *>(reinterpret_cast<char *>(s_x) + at[u]) = order_columns(v[u]);
+        for (int u = 0; u < U; ++u) {
+          if (i0 + u * kThreads >= total) break;
+          const u32x4 x = at[u] & 1 ? u32x4{0, 0, 0, 0} : v[u];
+          *reinterpret_cast<bf16x8 *>(reinterpret_cast<char *>(s_x) + (at[u] & ~1u)) = order_columns(x);
+        }
       }
 #pragma unroll
       for (int n = 0; n < NT; ++n)
 #pragma unroll
-        for (int i = 0; i < kTile * kPanelScales / kWave; ++i)
-          s_scale[wv][n][i * 2 + lane / kPanelScales][lane % kPanelScales] = sv[n][i];
+        for (int i = 0; i < N; ++i)
+          s_scale[wv][n][i * 2 + sr][sq] =
+              sq < nq && (n % NR) * kTile + i * 2 + sr < left
+                  ? __uint_as_float(sv[n][i] << (a.scale_bf16 ? 16 : 0)) : 0.f;
       __syncthreads();
       const int end = min(p0 + pcol, a.K);
       auto steps_of_panel = [&] {
@@ -392,22 +410,25 @@ __global__ __launch_bounds__(kThreads, 2) void w4_stream_kernel(W4Args a, int ks
 
 // Many token rows: a workgroup multiplies 64 of them with 256 weight rows (with
 // two matrices 128 of each), every wave 64 rows of its own, so that no code is
-// unpacked twice and a token row read from LDS meets four weight tiles.  The
-// -24 sums are made once, by the threads that bring the token rows to LDS.
+// unpacked twice.  The -24 sums are made once, by the threads that bring the
+// token rows to LDS.  A wave multiplies two of its four weight tiles at a time:
+// the sums of all four beside acc and the next step's operands would not fit
+// 256 registers, and reading the token rows from LDS twice costs less.
 // Both operands of the next step are requested before a step's products; the
 // token rows go through registers, where they take the codes' order, into the
 // other half of the LDS buffer.
 constexpr int kTileTok = 64, kTileStep = 128, kTileStride = kTileStep + 8;
-template <int MATS, int G32, bool SBF>
-__global__ __launch_bounds__(kThreads, 2) void w4_tile_kernel(W4Args a) {
-  constexpr int NT = 4, NR = NT / MATS, NTT = kTileTok / kTile, GS = 32 * G32;
-  constexpr int XC = kTileTok * kTileStep / 8 / kThreads;   // 16-byte chunks of x per thread
+constexpr int kTileThreads = 256, kTileWaves = kTileThreads / kWave, kTileWeights = 4;
+template <int MATS, int G32>
+__global__ __launch_bounds__(kTileThreads, 2) void w4_tile_kernel(W4Args a) {
+  constexpr int NT = kTileWeights, NP = 2, NR = NT / MATS, NTT = kTileTok / kTile, GS = 32 * G32;
+  constexpr int XC = (kTileTok * kTileStep / 8 + kTileThreads - 1) / kTileThreads;   // 16-byte chunks of x per thread
   __shared__ __align__(16) uint16_t s_x[2][kTileTok][kTileStride];
   __shared__ __align__(16) float s_start[2][4 / G32][kTileTok];
-  __shared__ float s_scale[kWaves][NT][kTile][kPanelScales + 1];
+  __shared__ float s_scale[kTileWaves][NT][kTile][kPanelScales + 1];
   const int lane = lane_id(), j = lane & 15, g = lane >> 4, tid = threadIdx.x;
   const int wv = uniform(tid / kWave);
-  const int rows = kWaves * NR * kTile, rt = (a.R + rows - 1) / rows;
+  const int rows = kTileWaves * NR * kTile, rt = (a.R + rows - 1) / rows;
   const int steps = (a.K + kTileStep - 1) / kTileStep, groups = a.K / GS;
   const Tiles tiles(a, kTileTok);
   // Consecutive workgroups run on the 8 XCDs in turn: each XCD gets a run of
@@ -429,17 +450,17 @@ __global__ __launch_bounds__(kThreads, 2) void w4_tile_kernel(W4Args a) {
 #pragma unroll
     for (int n = 0; n < MATS; ++n) {
       wb[n] = const_cast<char *>(uniform_ptr(static_cast<const char *>(a.w[n]) + first * wrow));
-      sb[n] = uniform_ptr(static_cast<const char *>(a.scale[n]) + first * groups * (SBF ? 2 : 4));
+      sb[n] = uniform_ptr(static_cast<const char *>(a.scale[n]) + first * groups * (a.scale_bf16 ? 2 : 4));
     }
     uint32_t wo[NR];
 #pragma unroll
     for (int n = 0; n < NR; ++n) wo[n] = (n * kTile + j) * wrow + g * 16;
     char *xb = const_cast<char *>(
         uniform_ptr(static_cast<const char *>(a.x) + (size_t)m0 * a.K * 2));
-    uint32_t xo[XC];   // token row tid / 16 + 16 i, chunk tid % 16
+    uint32_t xo[XC];   // token row tid / 16 + 32 i, chunk tid % 16
 #pragma unroll
     for (int i = 0; i < XC; ++i)
-      xo[i] = (uint32_t)min(tid / 16 + i * 16, ntok - 1) * a.K * 2 + tid % 16 * 16;
+      xo[i] = (uint32_t)min(tid / 16 + i * (kTileThreads / 16), ntok - 1) * a.K * 2 + tid % 16 * 16;
     u32x4 W[2][NT], X[XC];
     auto request_w = [&](int q, int s) {
       const int bytes = s < steps ? (int)(left * wrow) : 0, at = s < steps ? s * (kTileStep / 2) : 0;
@@ -459,85 +480,79 @@ __global__ __launch_bounds__(kThreads, 2) void w4_tile_kernel(W4Args a) {
 #pragma unroll
       for (int i = 0; i < XC; ++i) {
         const u32x4 v = ok ? X[i] : u32x4{0, 0, 0, 0};
-        const int row = tid / 16 + i * 16;
+        const int row = tid / 16 + i * (kTileThreads / 16);
+        if (row >= kTileTok) break;   // whole waves
         *reinterpret_cast<bf16x8 *>(&s_x[q][row][tid % 16 * 8]) = order_columns(v);
         const float sum = minus_24_sum<G32 * 4>(v);
         if (tid % (G32 * 4) == 0) s_start[q][tid % 16 / (G32 * 4)][row] = sum;
       }
     };
     auto put_scales = [&](int q0) {   // this wave's, of kPanelScales groups
+      constexpr int N = kTile * kPanelScales / kWave;
+      const int sr = lane / kPanelScales, sq = lane % kPanelScales;
 #pragma unroll 1
-      for (int n = 0; n < NT; ++n) {
-        constexpr int N = kTile * kPanelScales / kWave;
-        const void *from = n < NR ? sb[0] : sb[MATS - 1];
-        float v[N];
+      for (int n = 0; n < NT; ++n)
+        with_scales(n < NR ? sb[0] : sb[MATS - 1], a.scale_bf16, [&](auto *from, int shift) {
+          uint32_t v[N];
 #pragma unroll
-        for (int i = 0; i < N; ++i) {   // two rows at a time
-          const int r = n % NR * kTile + i * 2 + lane / kPanelScales, q = q0 + lane % kPanelScales;
-          const bool ok = q < groups && r < left;
-          const uint32_t at = ok ? r * groups + q : 0;
-          if constexpr (SBF) v[i] = bf16_to_f32(glob(static_cast<const uint16_t *>(from))[at]);
-          else v[i] = glob(static_cast<const float *>(from))[at];
-          v[i] = ok ? v[i] : 0.f;
-        }
+          for (int i = 0; i < N; ++i) {   // two rows at a time
+            const int r = n % NR * kTile + i * 2 + sr;
+            v[i] = from[q0 + sq < groups && r < left ? r * groups + q0 + sq : 0];
+          }
 #pragma unroll
-        for (int i = 0; i < N; ++i)
-          s_scale[wv][n][i * 2 + lane / kPanelScales][lane % kPanelScales] = v[i];
-      }
+          for (int i = 0; i < N; ++i) {
+            const bool ok = q0 + sq < groups && n % NR * kTile + i * 2 + sr < left;
+            s_scale[wv][n][i * 2 + sr][sq] = ok ? __uint_as_float(v[i] << shift) : 0.f;
+          }
+        });
     };
-    f32x4 acc[NT][NTT] = {};
+    float acc[NT][NTT][4] = {};
     const Magic magic;
     auto multiply = [&](int q, int s) {
       const int q0 = s * (4 / G32) % kPanelScales;
 #pragma unroll
       for (int n = 0; n < NT; ++n) columns_together(W[q][n]);
 #pragma unroll
-      for (int i = 0; i < 4 / G32; ++i) {
-        // The shortest groups take two token tiles at a time, whose sums and the
-        // group's unpacked weights fit the registers beside acc.
-        constexpr int TP = G32 == 1 ? 2 : NTT;
-        bf16x8 w[NT];
-        if constexpr (G32 == 1)
+      for (int i = 0; i < 4 / G32; ++i)
 #pragma unroll
-          for (int n = 0; n < NT; ++n) w[n] = codes_to_bf16(W[q][n][i], magic);
+        for (int n0 = 0; n0 < NT; n0 += NP) {
+          f32x4 p[NP][NTT];
 #pragma unroll
-        for (int t0 = 0; t0 < NTT; t0 += TP) {
-          f32x4 p[NT][TP];
+          for (int t = 0; t < NTT; ++t) {   // lane group g: tokens 4 g .. 4 g + 3 of the tile
+            p[0][t] = *reinterpret_cast<const f32x4 *>(&s_start[q][i][t * kTile + g * 4]);
 #pragma unroll
-          for (int t = 0; t < TP; ++t) {   // lane group g: tokens 4 g .. 4 g + 3 of the tile
-            p[0][t] = *reinterpret_cast<const f32x4 *>(&s_start[q][i][(t0 + t) * kTile + g * 4]);
-#pragma unroll
-            for (int n = 1; n < NT; ++n) p[n][t] = p[0][t];
+            for (int n = 1; n < NP; ++n) p[n][t] = p[0][t];
           }
 #pragma unroll
-          for (int m = 0; m < G32; ++m) {
-            bf16x8 xv[TP];
+          for (int m = i * G32; m < (i + 1) * G32; ++m) {
+            bf16x8 xv[NTT];
 #pragma unroll
-            for (int t = 0; t < TP; ++t)
-              xv[t] = *reinterpret_cast<const bf16x8 *>(
-                  &s_x[q][(t0 + t) * kTile + j][(i * G32 + m) * 32 + g * 8]);
+            for (int t = 0; t < NTT; ++t)
+              xv[t] = *reinterpret_cast<const bf16x8 *>(&s_x[q][t * kTile + j][m * 32 + g * 8]);
 #pragma unroll
-            for (int n = 0; n < NT; ++n) {
-              if constexpr (G32 > 1) w[n] = codes_to_bf16(W[q][n][i * G32 + m], magic);
+            for (int n = 0; n < NP; ++n) {
+              const bf16x8 w = codes_to_bf16(W[q][n0 + n][m], magic);
 #pragma unroll
-              for (int t = 0; t < TP; ++t)
-                p[n][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xv[t], w[n], p[n][t], 0, 0, 0);
+              for (int t = 0; t < NTT; ++t)
+                p[n][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xv[t], w, p[n][t], 0, 0, 0);
             }
           }
 #pragma unroll
-          for (int n = 0; n < NT; ++n) {
-            const float sc = s_scale[wv][n][j][q0 + i];
+          for (int n = 0; n < NP; ++n) {
+            const float sc = s_scale[wv][n0 + n][j][q0 + i];
 #pragma unroll
-            for (int t = 0; t < TP; ++t) {
-              acc[n][t0 + t] += sc * p[n][t];
-              // here and now: left to the end of the step, all groups' sums
-              // would have to be kept
-              asm volatile("" : "+v"(acc[n][t0 + t]));
-            }
+            for (int t = 0; t < NTT; ++t)
+#pragma unroll
+              for (int r = 0; r < 4; ++r) {
+                float &v = acc[n0 + n][t][r];
+                v = __builtin_fmaf(sc, p[n][t][r], v);
+                // here and now: left to the end of the step, all groups' sums
+                // would have to be kept
+                asm volatile("" : "+v"(v));
+              }
           }
           __builtin_amdgcn_sched_barrier(0);
         }
-      }
     };
     __syncthreads();   // the last item's token rows have been read
     request_w(0, 0);
@@ -553,6 +568,7 @@ __global__ __launch_bounds__(kThreads, 2) void w4_tile_kernel(W4Args a) {
           if (s + q >= steps) return;
           request_x(s + q + 1);
           request_w(q ^ 1, s + q + 1);
+          __builtin_amdgcn_sched_barrier(0);   // not among the products
           multiply(q, s + q);
           if ((s + q + 1) * (4 / G32) % kPanelScales == 0) put_scales((s + q + 1) * (4 / G32));
           put_x(q ^ 1, s + q + 1);
@@ -578,66 +594,77 @@ __global__ __launch_bounds__(kThreads, 2) void w4_tile_kernel(W4Args a) {
 
 namespace {
 
+// Row tiles of the matrices at most: with offsets, every matrix may end inside
+// one.
+int64_t row_tiles(const W4Args &a, int rows) {
+  return a.offset ? a.M / rows + (a.n < a.M ? a.n : a.M) : (a.M + rows - 1) / rows;
+}
+
+dim3 grid_of(int64_t items) { return dim3((unsigned)(items < (1 << 20) ? items : 1 << 20)); }
+
 // K parts of a workgroup, at most `want`: a panel holds a round of the ring.
-int k_parts(const W4Args &a, int ntt, int step, int want) {
-  const int rows = a.M < kTile * ntt ? a.M : kTile * ntt;
+int k_parts(const W4Args &a, int ntt, int want) {
+  const int rows = a.M < kTile * ntt ? a.M : kTile * ntt, round = kRingColumns;
   int ks = want;
-  while (ks > 1 && (ks * step > kPanelScales * a.group || ks * step > kPanelWords * ntt * 2 / rows - 8))
+  while (ks > 1 && (ks * round > kPanelScales * a.group || ks * round > kPanelWords * ntt * 2 / rows - 8))
     ks /= 2;
   return ks;
 }
 
-template <int MATS, int NR, int NTT, int D, int CH>
-hipError_t stream_grouped(const W4Args &a, int want, hipStream_t s) {
-  const int ks = k_parts(a, NTT, D * CH * 128, want);
-  const int tr = kTile * NTT, rows = kWaves / ks * NR * kTile;
-  const int64_t tiles = a.offset ? a.M / tr + (a.n < a.M ? a.n : a.M) : (a.M + tr - 1) / tr;
-  const int64_t items = tiles * ((a.R + rows - 1) / rows);   // the most there can be
-  const dim3 grid((unsigned)(items < (1 << 20) ? items : 1 << 20)), block(kThreads);
-#define W4_STREAM(G, B) \
-  hipLaunchKernelGGL((w4_stream_kernel<MATS, NR, NTT, G, B, D, CH>), grid, block, 0, s, a, ks)
-  if (a.scale_bf16) {
-    if (a.group == 32) W4_STREAM(1, true);
-    else if (a.group == 64) W4_STREAM(2, true);
-    else W4_STREAM(4, true);
-  } else {
-    if (a.group == 32) W4_STREAM(1, false);
-    else if (a.group == 64) W4_STREAM(2, false);
-    else W4_STREAM(4, false);
-  }
-#undef W4_STREAM
+template <int MATS, int NR, int NTT, bool KEEP>
+hipError_t stream(const W4Args &a, int want, hipStream_t s) {
+  const int ks = k_parts(a, NTT, want), rows = kWaves / ks * NR * kTile;
+  const dim3 grid = grid_of(row_tiles(a, kTile * NTT) * ((a.R + rows - 1) / rows));
+  auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, s, a, ks); };
+  if (a.group == 32) launch(w4_stream_kernel<MATS, NR, NTT, 1, KEEP>);
+  else if (a.group == 64) launch(w4_stream_kernel<MATS, NR, NTT, 2, KEEP>);
+  else launch(w4_stream_kernel<MATS, NR, NTT, 4, KEEP>);
   return hipGetLastError();
 }
 
 template <int MATS>
-hipError_t tile_grouped(const W4Args &a, hipStream_t s) {
-  const int rows = kWaves * 4 / MATS * kTile;
-  const int64_t tiles = a.offset ? a.M / kTileTok + (a.n < a.M ? a.n : a.M) : (a.M + kTileTok - 1) / kTileTok;
-  const int64_t items = (tiles * ((a.R + rows - 1) / rows) + 7) / 8 * 8;   // the most there can be
-  const dim3 grid((unsigned)(items < (1 << 20) ? items : 1 << 20)), block(kThreads);
-#define W4_TILE(G, B) hipLaunchKernelGGL((w4_tile_kernel<MATS, G, B>), grid, block, 0, s, a)
-  if (a.scale_bf16) {
-    if (a.group == 32) W4_TILE(1, true);
-    else if (a.group == 64) W4_TILE(2, true);
-    else W4_TILE(4, true);
-  } else {
-    if (a.group == 32) W4_TILE(1, false);
-    else if (a.group == 64) W4_TILE(2, false);
-    else W4_TILE(4, false);
-  }
-#undef W4_TILE
+hipError_t tile(const W4Args &a, hipStream_t s) {
+  const int rows = kTileWaves * kTileWeights / MATS * kTile;
+  const int64_t items = row_tiles(a, kTileTok) * ((a.R + rows - 1) / rows);
+  const dim3 grid = grid_of((items + 7) / 8 * 8);
+  auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(kTileThreads), 0, s, a); };
+  if (a.group == 32) launch(w4_tile_kernel<MATS, 1>);
+  else if (a.group == 64) launch(w4_tile_kernel<MATS, 2>);
+  else launch(w4_tile_kernel<MATS, 4>);
   return hipGetLastError();
+}
+
+template <int MATS>
+hipError_t run(const W4Args &a, hipStream_t s) {
+  const int blocks = (a.R + 255) / 256 * MATS;
+  if (a.offset) {
+    // The mean rows of a matrix decide, us, streamed | tiled: 64 experts of 2 x
+    // 1280 x 2048, 54 | 98 at 12 rows, 88 | 99 at 24, 124 | 106 at 36; of 2048 x
+    // 1280, 44 | 43 at 12 rows, 65 | 56 at 24.
+    const int64_t mean = a.M / a.n;
+    if (mean > (MATS == 2 ? 28 : 14)) return tile<MATS>(a, s);
+    // Few workgroups: K over two waves (8 rows of 2 x 2048 x 7168: 31.7 -> 27.8 us).
+    // Many, of one matrix: four weight tiles per wave (82 experts of 4096 x 1536:
+    // 81 -> 75 us; but 48 of 2048 x 1280 34 -> 41).
+    const int64_t groups = row_tiles(a, kTile) * ((a.R + 63) / 64);
+    if (MATS == 1 && groups >= 5120) return stream<1, 4, 1, false>(a, 1, s);
+    return stream<MATS, 1, 1, false>(a, groups < 512 ? 2 : 1, s);
+  }
+  if ((int64_t)((a.M + 63) / 64) * blocks >= 256) return tile<MATS>(a, s);
+  // few tiles of a matrix: K over four waves, or two, so that all CUs take part
+  const int64_t tiles = (int64_t)((a.R + 15) / 16) * ((a.M + 15) / 16);
+  const int ks = tiles < 512 ? 4 : tiles < 704 ? 2 : 1;
+  if (a.M <= kTile) return stream<MATS, 1, 1, false>(a, ks, s);
+  // two token tiles per pass over the weights, us, one | two: 4096 x 4096, 22.8 |
+  // 25.8 at 128 rows, 38.9 | 34.4 at 256; two matrices 53 | 64 at 200
+  if (MATS == 1 && a.M > 160) return stream<1, 1, 2, true>(a, ks, s);
+  return stream<MATS, 1, 1, true>(a, ks, s);
 }
 
 }  // namespace
 
 hipError_t launch_w4(const W4Args &a, int mats, hipStream_t s) {
-  const int per = a.offset ? (a.M + a.n - 1) / a.n : a.M;   // rows of a matrix on average
-  const int ks = a.offset ? 1 : 4;
-  if (per > 64) return mats == 2 ? tile_grouped<2>(a, s) : tile_grouped<1>(a, s);
-  if (mats == 2)
-    return per <= 16 ? stream_grouped<2, 1, 1, 2, 2>(a, ks, s) : stream_grouped<2, 1, 2, 2, 2>(a, ks, s);
-  return per <= 16 ? stream_grouped<1, 1, 1, 2, 2>(a, ks, s) : stream_grouped<1, 1, 4, 2, 2>(a, ks, s);
+  return mats == 2 ? run<2>(a, s) : run<1>(a, s);
 }
 
 }  // namespace deamoe
