@@ -315,24 +315,23 @@ def _call(fn, dev: int, stream, args) -> int:
     if dev != torch.cuda.current_device():
         with torch.cuda.device(dev):
             return _call(fn, dev, stream, args)
-    return fn(*args, torch.cuda.current_stream().cuda_stream if stream is None else stream.cuda_stream)
+    # the raw handle: a torch.cuda.Stream made for the call costs more than the launch
+    return fn(*args, torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream)
 
 
 def _run(fn, dev: int, stream, *args):
     _check(_call(fn, dev, stream, args), fn.__name__)
 
 
-def _run_with_workspace(fn, dev: int, stream, ws, nbytes, *args):
-    """The same for a call that may need a workspace of nbytes() (its last two arguments): the given
-    one, or one of torch's for the stream that the call runs on, asked for if the call wants it."""
-    if ws is not None and (ws.get_device() != dev or not ws.is_contiguous()):
-        raise DeamoeError(ERR_WORKSPACE, f"{fn.__name__}: workspace is not contiguous, or not on device {dev}")
-    status = _call(fn, dev, stream, (*args, _ptr(ws), 0 if ws is None else ws.numel() * ws.element_size()))
-    if status == ERR_WORKSPACE and ws is None:
+def _run_with_workspace(fn, dev: int, stream, ws, nbytes: int, *args):
+    """The same for a call whose last two arguments are its workspace: the given one, or one of torch's
+    for the stream that the call runs on."""
+    if ws is None and nbytes and dev >= 0:
         with contextlib.nullcontext() if stream is None else torch.cuda.stream(stream):
-            ws = torch.empty(nbytes(), dtype=torch.uint8, device=f"cuda:{dev}")
-        status = _call(fn, dev, stream, (*args, ws.data_ptr(), ws.numel()))
-    _check(status, fn.__name__)
+            ws = torch.empty(nbytes, dtype=torch.uint8, device=torch.device("cuda", dev))
+    elif ws is not None and (ws.get_device() != dev or not ws.is_contiguous()):
+        raise DeamoeError(ERR_WORKSPACE, f"{fn.__name__}: workspace is not contiguous, or not on device {dev}")
+    _run(fn, dev, stream, *args, _ptr(ws), 0 if ws is None else ws.numel() * ws.element_size())
 
 
 def _bytes(fn, *args) -> int:
@@ -363,7 +362,7 @@ def deamoe_dispatch(ids, x, offset, pair, row, xs=None, ws=None, stream=None):
         act, h = _act(what, x), _rows(what, x, "x")[1]
         _fits(what, dev, ("x", x, x.dtype, (T, h)), ("xs", xs, x.dtype, (T * k, h)))
     _run_with_workspace(lib().deamoe_dispatch, dev, stream, ws,
-                        lambda: deamoe_dispatch_workspace_bytes(T, k, n), T, k, n, h, act,
+                        deamoe_dispatch_workspace_bytes(T, k, n), T, k, n, h, act,
                         ids.data_ptr(), x.data_ptr() if xs is not None else None, offset.data_ptr(),
                         pair.data_ptr(), row.data_ptr(), _ptr(xs))
 
@@ -464,7 +463,7 @@ def deamoe_prenorm_backward(x, w, du, dx, dw, dres=None, eps: float = 1e-6, ws=N
     if dres is not None:
         _fits(what, dev, ("dres", dres, dt, (T, h)))
     _run_with_workspace(lib().deamoe_prenorm_backward, dev, stream, ws,
-                        lambda: deamoe_norm_workspace_bytes(T, h), T, h, act, eps, x.data_ptr(),
+                        deamoe_norm_workspace_bytes(T, h), T, h, act, eps, x.data_ptr(),
                         w.data_ptr(), du.data_ptr(), _ptr(dres), dx.data_ptr(), dw.data_ptr())
 
 
@@ -512,7 +511,7 @@ def deamoe_postnorm_backward(y, w, dz, dx, dy, dw, gate=None, dgate=None, res_sc
         _fits(what, dev, ("z", z, dt, full), ("w_next", w_next, dt, vec), ("du", du, dt, full),
               ("dw_next", dw_next, f32, vec))
     _run_with_workspace(lib().deamoe_postnorm_backward, dev, stream, ws,
-                        lambda: deamoe_norm_workspace_bytes(T, h), T, h, act, eps, res_scale, mode,
+                        deamoe_norm_workspace_bytes(T, h), T, h, act, eps, res_scale, mode,
                         y.data_ptr(), w.data_ptr(), _ptr(gate), _ptr(z), _ptr(w_next), dz.data_ptr(),
                         _ptr(du), dx.data_ptr(), dy.data_ptr(), dw.data_ptr(), _ptr(dgate), _ptr(dw_next))
 
