@@ -16,6 +16,25 @@ namespace deamoe {
 
 namespace {
 
+template <int CTRL>
+__device__ inline float dpp(float v) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, false));
+}
+
+// The sum over a row of 16 lanes, on all of them: lane i adds lane i ^ 1, i ^ 2,
+// then a lane of the other quad, of the other half.  In registers: a shuffle
+// through LDS per step took a quarter of a row's time.
+__device__ inline float sum16(float v) {
+  v += dpp<0xb1>(v);    // quad_perm [1, 0, 3, 2]
+  v += dpp<0x4e>(v);    // quad_perm [2, 3, 0, 1]
+  v += dpp<0x141>(v);   // row_half_mirror
+  v += dpp<0x140>(v);   // row_mirror
+  return v;
+}
+__device__ inline float lane_value(float v, int lane) {
+  return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), lane));
+}
+
 // Sums of N values over the workgroup, the same on every thread.  Two
 // reductions in a row use different halves of `s`, so that one barrier each is
 // enough.
@@ -25,21 +44,19 @@ struct Reduce {
   int flip = 0;
   template <int N>
   __device__ void sum(float (&v)[N]) {
-    const int waves = blockDim.x / kWave;
+    const int waves = blockDim.x / kWave, lane = threadIdx.x % kWave;
 #pragma unroll
-    for (int i = 0; i < N; ++i)
-#pragma unroll
-      for (int o = kWave / 2; o; o /= 2) v[i] += __shfl_xor(v[i], o);
+    for (int i = 0; i < N; ++i) {
+      v[i] = sum16(v[i]);
+      v[i] = (lane_value(v[i], 0) + lane_value(v[i], 16)) + (lane_value(v[i], 32) + lane_value(v[i], 48));
+    }
     if (waves == 1) return;
-    if (threadIdx.x % kWave == 0)
+    if (lane == 0)
 #pragma unroll
       for (int i = 0; i < N; ++i) s[flip][i][threadIdx.x / kWave] = v[i];
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      v[i] = 0.f;
-      for (int w = 0; w < waves; ++w) v[i] += s[flip][i][w];
-    }
+    for (int i = 0; i < N; ++i) v[i] = sum16(lane % 16 < waves ? s[flip][i][lane % 16] : 0.f);
     flip ^= 1;
   }
 };
@@ -166,11 +183,9 @@ template <bool F32, int N, int MODE>
 struct BackwardRows {   // what one row reads
   Row<F32, MODE != NORM_POST ? N : 0> z, du;
   Row<F32, MODE != NORM_PRE ? N : 0> y;
-  Row<F32, N> dz, gate;
+  Row<F32, N> dz;
   __device__ BackwardRows(const NormBackwardArgs &a, int t)
-      : z(a.z, t, a.h), du(a.du, t, a.h), y(a.y, t, a.h), dz(a.dz ? a.dz : a.du, t, a.h),
-        gate(a.gate_mode == DEAMOE_GATE_NONE ? (a.w ? a.w : a.w_next) : a.gate,
-             a.gate_mode == DEAMOE_GATE_FULL ? t : 0, a.h) {}
+      : z(a.z, t, a.h), du(a.du, t, a.h), y(a.y, t, a.h), dz(a.dz ? a.dz : a.du, t, a.h) {}
 };
 
 template <bool F32, int N, int MAXG, int MODE>
@@ -200,6 +215,8 @@ __global__ __launch_bounds__(MAXG) void norm_backward_kernel(NormBackwardArgs a)
   for (int t = blockIdx.x; t < a.T; t += gridDim.x) {
     const bool first = t == (int)blockIdx.x;
     const BackwardRows<F32, N, MODE> r = next;
+    const Row<F32, POST ? N : 0> gate(a.gate_mode == DEAMOE_GATE_NONE ? a.w : a.gate,
+                                      a.gate_mode == DEAMOE_GATE_FULL ? t : 0, h);
     // the next row is on its way while this one waits for its sums
     if (t + (int)gridDim.x < a.T) next = BackwardRows<F32, N, MODE>(a, t + gridDim.x);
     float s1[3] = {0.f, 0.f, 0.f};   // z^2, du w' z, y^2
@@ -242,7 +259,7 @@ __global__ __launch_bounds__(MAXG) void norm_backward_kernel(NormBackwardArgs a)
 #pragma unroll
         for (int e = 0; e < V; ++e) dn[e] = dh[i][e];
         if (a.gate_mode != DEAMOE_GATE_NONE) {
-          const Chunk<F32> g = r.gate.get(i, c);
+          const Chunk<F32> g = gate.get(i, c);
 #pragma unroll
           for (int e = 0; e < V; ++e) dn[e] *= g.at(e);
         }
@@ -275,7 +292,7 @@ __global__ __launch_bounds__(MAXG) void norm_backward_kernel(NormBackwardArgs a)
           g[e] = d[e] * (yv.at(e) * ry * wv.at(e));
         }
         if (a.gate_mode != DEAMOE_GATE_NONE) {
-          const Chunk<F32> gv = r.gate.get(i, c);
+          const Chunk<F32> gv = gate.get(i, c);
 #pragma unroll
           for (int e = 0; e < V; ++e) dn[e] *= gv.at(e);
           if (a.gate_mode == DEAMOE_GATE_FULL)
@@ -346,8 +363,11 @@ __global__ __launch_bounds__(1024) void column_sum_kernel(ColumnSumArgs a) {
 
 namespace {
 
-// Threads and held chunks per thread for a row: up to two chunks of 16 bytes
-// each and 1024 threads; wider rows are not held.
+// Threads and held chunks of 16 bytes per thread for a row: as few threads as
+// hold it with two chunks each while that leaves several rows per CU; from 4097
+// bf16 columns on one chunk each, in 1024 threads (the gradient of 2048 rows of
+// 7168: 71 us with 512 threads of two chunks, 50 with these); rows wider than
+// 2048 chunks are not held.
 struct Shape {
   int threads, held;
 };
@@ -357,7 +377,7 @@ Shape shape_of(int h, int act_f32) {
   if (chunks <= 128) return {128, 1};
   if (chunks <= 256) return {256, 1};
   if (chunks <= 512) return {256, 2};
-  if (chunks <= 1024) return {512, 2};
+  if (chunks <= 1024) return {1024, 1};
   if (chunks <= 2048) return {1024, 2};
   return {1024, 0};
 }
@@ -383,8 +403,10 @@ hipError_t with_shape(Shape sh, bool f32, F f) {
   using std::integral_constant;
   auto typed = [&](auto F32) {
     if (sh.held == 0) return f(F32, integral_constant<int, 0>{}, integral_constant<int, 1024>{});
-    if (sh.threads == 1024)
+    if (sh.threads == 1024 && sh.held == 2)
       return f(F32, integral_constant<int, 2>{}, integral_constant<int, 1024>{});
+    if (sh.threads == 1024) return f(F32, integral_constant<int, 1>{}, integral_constant<int, 1024>{});
+    // bounded as for 512 threads: 256 registers, two waves per SIMD
     if (sh.held == 2) return f(F32, integral_constant<int, 2>{}, integral_constant<int, 512>{});
     return f(F32, integral_constant<int, 1>{}, integral_constant<int, 256>{});
   };
@@ -393,11 +415,12 @@ hipError_t with_shape(Shape sh, bool f32, F f) {
 
 }  // namespace
 
-// As many workgroups as run at once (eight waves on each of the 256 CUs, one
-// workgroup at least), and of those as many as share the rows evenly.
+// As many workgroups as run at once (eight waves on each of the 256 CUs; one
+// workgroup at least; 1024 at most, whose parts are summed afterwards), and of
+// those as many as share the rows evenly.
 int norm_backward_blocks(int T, int h) {
   const int threads = shape_of(h, 0).threads;   // the smaller of the two types' shapes
-  const int most = threads >= 512 ? 256 : 131072 / threads;
+  const int most = threads >= 512 ? 256 : threads >= 128 ? 131072 / threads : 1024;
   if (T <= most) return T;
   const int rows = (T + most - 1) / most;
   return (T + rows - 1) / rows;
