@@ -292,7 +292,8 @@ int deamoe_combine_backward(int32_t T, int32_t k, int32_t h, int32_t act_dtype,
  * x meet matrix e (the lists of deamoe_dispatch); rows outside [offset[0],
  * offset[n]) are left as they were; values outside [0, M] are taken as the
  * nearer end.  NULL: one matrix (n == 1) for all rows.
- * An infinity or NaN in a row of x makes that row of the output NaN.
+ * An infinity or NaN in a row of x makes that row of the output NaN; finite
+ * values may where 31 times the sum of a group's |x| passes the fp32 range.
  * K a multiple of group; group 32, 64 or 128; any R; n <= DEAMOE_MAX_EXPERTS;
  * codes and x 16-byte aligned. */
 typedef struct {

@@ -457,10 +457,10 @@ __global__ __launch_bounds__(kTileThreads, 2) void w4_tile_kernel(W4Args a) {
     for (int n = 0; n < NR; ++n) wo[n] = (n * kTile + j) * wrow + g * 16;
     char *xb = const_cast<char *>(
         uniform_ptr(static_cast<const char *>(a.x) + (size_t)m0 * a.K * 2));
-    uint32_t xo[XC];   // token row tid / 16 + 32 i, chunk tid % 16
+    uint32_t xo[XC];   // token row tid / 16 + 16 i
 #pragma unroll
     for (int i = 0; i < XC; ++i)
-      xo[i] = (uint32_t)min(tid / 16 + i * (kTileThreads / 16), ntok - 1) * a.K * 2 + tid % 16 * 16;
+      xo[i] = (uint32_t)min(tid / 16 + i * (kTileThreads / 16), ntok - 1) * a.K * 2;
     u32x4 W[2][NT], X[XC];
     auto request_w = [&](int q, int s) {
       const int bytes = s < steps ? (int)(left * wrow) : 0, at = s < steps ? s * (kTileStep / 2) : 0;
@@ -469,11 +469,10 @@ __global__ __launch_bounds__(kTileThreads, 2) void w4_tile_kernel(W4Args a) {
         W[q][n] = __builtin_amdgcn_raw_buffer_load_b128(
             __builtin_amdgcn_make_buffer_rsrc(wb[n / NR], 0, bytes, 0x00027000), wo[n % NR], at, 0);
     };
-    auto request_x = [&](int s) {
-      const bool ok = s * kTileStep + tid % 16 * 8 < a.K;
+    auto request_x = [&](int s) {   // chunk tid % 16 of the step; past the row's end its first
+      const uint32_t col = s * kTileStep + tid % 16 * 8, at = col < (uint32_t)a.K ? col * 2 : 0u;
 #pragma unroll
-      for (int i = 0; i < XC; ++i)
-        X[i] = *gptr(xb + xo[i] + (ok ? (uint32_t)s * kTileStep * 2 : 0u));
+      for (int i = 0; i < XC; ++i) X[i] = *gptr(xb + (xo[i] + at));
     };
     auto put_x = [&](int q, int s) {
       const bool ok = s * kTileStep + tid % 16 * 8 < a.K;

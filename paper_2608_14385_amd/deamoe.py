@@ -294,6 +294,8 @@ class Layer:
 def _fits(what: str, dev: int, *tensors):
     """Every (name, tensor, dtype, shape) has that type and shape, is contiguous and on device `dev`."""
     for name, t, dtype, shape in tensors:
+        if t is None:
+            raise DeamoeError(ERR_INVALID, f"{what}: {name} is needed")
         if t.dtype is not dtype or t.shape != shape or t.get_device() != dev or not t.is_contiguous():
             raise DeamoeError(ERR_INVALID, f"{what}: {name} is {t.dtype} {tuple(t.shape)} with strides "
                               f"{t.stride()} on {t.device}; needed is {dtype} {tuple(shape)}, contiguous, "
@@ -341,8 +343,9 @@ def _bytes(fn, *args) -> int:
 
 
 def _rows(what: str, t: torch.Tensor, name: str) -> tuple:
-    if t.dim() != 2:
-        raise DeamoeError(ERR_INVALID, f"{what}: {name} has {t.dim()} dimensions, needed are 2")
+    if t is None or t.dim() != 2:
+        raise DeamoeError(ERR_INVALID, f"{what}: {name} is "
+                          f"{'missing' if t is None else tuple(t.shape)}, needed are two dimensions")
     return t.shape
 
 
@@ -359,7 +362,7 @@ def deamoe_dispatch(ids, x, offset, pair, row, xs=None, ws=None, stream=None):
     _fits(what, dev, ("ids", ids, i32, (T, k)), ("offset", offset, i32, (n + 1,)),
           ("pair", pair, i32, (T * k,)), ("row", row, i32, (T, k)))
     if xs is not None:
-        act, h = _act(what, x), _rows(what, x, "x")[1]
+        h, act = _rows(what, x, "x")[1], _act(what, x)
         _fits(what, dev, ("x", x, x.dtype, (T, h)), ("xs", xs, x.dtype, (T * k, h)))
     _run_with_workspace(lib().deamoe_dispatch, dev, stream, ws,
                         deamoe_dispatch_workspace_bytes(T, k, n), T, k, n, h, act,
@@ -555,9 +558,12 @@ class Block:
         self.layer, self.w_pre, self.w_post, self.gate = layer, w_pre, w_post, gate
         self.res_scale, self.eps, self.w_next = res_scale, eps, w_next
 
-    def __call__(self, x, u=None, **kw):
+    def __call__(self, x, u=None, stream=None, **kw):
         """z, or with w_next (z, u): u is the next block's normed input, which its call takes in
-        place of norming x again.  Keyword arguments go to the layer."""
+        place of norming x again.  Further keyword arguments go to the layer."""
+        if stream is not None:
+            with torch.cuda.stream(stream):
+                return self(x, u, **kw)
         if u is None:
             u = torch.empty_like(x)
             deamoe_prenorm(x, self.w_pre, u, eps=self.eps)

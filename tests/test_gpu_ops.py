@@ -245,6 +245,89 @@ def test_w4_experts(T, k, n, R_, K, group, kind):
             close(z[at], want, bound, BF, f"swiglu of expert {e}")
 
 
+@pytest.mark.parametrize("scale", [F32, BF])
+@pytest.mark.parametrize("M,R_,K,group", [
+    (2048, 2050, 1152, 128), (1100, 4000, 320, 64), (1030, 4097, 2080, 32),   # 64-row tiles
+    (160, 700, 2112, 64), (161, 1500, 4128, 32), (250, 2100, 1152, 128),      # one and two token tiles
+    (16, 8300, 1056, 32), (12, 10000, 192, 64), (9, 12001, 4224, 128),        # K over four, two waves, one
+])
+def test_w4_linear_by_kernel(M, R_, K, group, scale):
+    """Sizes on either side of what chooses the kernel and its split, with a K that ends inside a step
+    and, for small groups, more scales than stand in LDS at once."""
+    say(f"[gpu] w4 choice M={M} R={R_} K={K} group={group} {scale}")
+    test_w4_linear(M, R_, K, group, scale)
+
+
+def sampled_experts(offset, M, n, R_, K, group, g, scale=F32, mats=2):
+    """One call over given offsets, checked on the rows around every few matrices' ends."""
+    mat = [matrix(g, n, R_, K=K, group=group, scale=scale) for _ in range(mats)]
+    x, y = normal(g, M, K, dtype=BF), torch.full((M, R_), 9.0, dtype=BF, device="cuda")
+    if mats == 2:
+        D.deamoe_w4_swiglu(x, *mat[0], *mat[1], y, offset=offset)
+    else:
+        D.deamoe_w4_linear(x, *mat[0], y, offset=offset)
+    o = offset.tolist()
+    assert bool((y[o[-1]:] == 9.0).all()) and bool((y[:o[0]] == 9.0).all())
+    held = [e for e in range(n) if o[e] < o[e + 1]]
+    for e in sorted({held[0], held[-1], *held[::max(len(held) // 6, 1)]}):
+        rows = torch.unique(torch.cat([torch.arange(o[e], min(o[e] + 40, o[e + 1])),
+                                       torch.arange(max(o[e + 1] - 40, o[e]), o[e + 1])])).cuda()
+        want, bound = R.w4_product(x[rows], mat[0][0][e], mat[0][1][e], group)
+        if mats == 2:
+            want, bound = R.swiglu(want, bound, *R.w4_product(x[rows], mat[1][0][e], mat[1][1][e], group))
+        close(y[rows], want, bound, BF, f"matrix {e}")
+
+
+@pytest.mark.parametrize("scale", [F32, BF])
+@pytest.mark.parametrize("mats", [1, 2])
+@pytest.mark.parametrize("T,k,n,R_,K,group,kind", [
+    (60, 5, 64, 4100, 160, 32, "topk"), (60, 5, 64, 4100, 1152, 128, "topk"), (60, 5, 64, 4100, 320, 64, "stray"),
+    (20, 2, 4, 70, 2144, 32, "any"),                                      # few workgroups
+    (900, 4, 2047, 65, 1056, 32, "any"), (4000, 8, 100, 260, 2080, 32, "topk"),
+    (2000, 2, 64, 130, 192, 64, "stray"), (500, 2, 16, 300, 4224, 128, "any"), (1300, 1, 1, 100, 128, 64, "any"),
+])
+def test_w4_experts_by_kernel(T, k, n, R_, K, group, kind, mats, scale):
+    say(f"[gpu] w4 experts choice T={T} k={k} n={n} R={R_} K={K} group={group} {kind} {mats} {scale}")
+    g = gen(T + n)
+    offset = Sorted(ids_of(g, T, k, n, kind), n).offset
+    sampled_experts(offset, T * k, n, R_, K, group, g, scale, mats)
+
+
+def test_w4_uneven_experts():
+    """Routing that the mean number of rows says nothing about: one matrix with nearly all rows, and
+    rows before the first matrix and behind the last."""
+    g = gen(3)
+    for n, M, mats in ((200, 2500, 2), (200, 2500, 1), (6, 2500, 2)):
+        o = torch.full((n + 1,), 2400, dtype=I32, device="cuda")
+        o[:4] = torch.tensor([5, 5, 6, 23], dtype=I32)
+        o[-2:] = torch.tensor([2400, 2431], dtype=I32)
+        say(f"[gpu] w4 uneven n={n} M={M} {mats}")
+        sampled_experts(o, M, n, 150, 256, 64, g, mats=mats)
+
+
+def test_w4_more_items_than_workgroups():
+    """Grids end at 2^20 workgroups, which walk over the rest."""
+    g = gen(5)
+    n, M, R_, K = 2048, 3000, 65536, 32
+    say(f"[gpu] w4 swiglu of {n} x {R_} x {K}")
+    offset = Sorted(ids_of(g, M, 1, n, "any"), n).offset
+    sampled_experts(offset, M, n, R_, K, 32, g)
+
+
+def test_w4_rows_past_four_gigabytes():
+    g, n, M, K = gen(6), 3, 1 << 26, 64
+    say(f"[gpu] w4 of {M * K * 2 / 2**30:.0f} GiB of rows")
+    codes, s = matrix(g, n, 1, K=K, group=32)
+    x = normal(g, 1 << 16, K, dtype=BF).repeat(M >> 16, 1)
+    offset = torch.tensor([0, 33, (1 << 25) + 7, M], dtype=I32, device="cuda")
+    y = torch.empty(M, 1, dtype=BF, device="cuda")
+    D.deamoe_w4_linear(x, codes, s, y, offset=offset)
+    for e, (lo, hi) in enumerate(((0, 33), (33, (1 << 25) + 7), ((1 << 25) + 7, M))):
+        for at in (slice(lo, min(lo + 100, hi)), slice(max(hi - 100, lo), hi)):
+            want, bound = R.w4_product(x[at], codes[e], s[e], 32)
+            close(y[at], want, bound, BF, f"matrix {e}")
+
+
 def test_w4_offsets_outside_the_rows():
     """Offsets past the rows are taken as their end, rows before the first stay as they were."""
     g = gen(8)
@@ -280,6 +363,8 @@ def test_w4_keeps_bad_rows_to_themselves(M):
 EPS = 1e-6
 NORM_SHAPES = [(1, 1), (3, 7), (16, 7168), (5, 64), (130, 1000), (64, 4096), (33, 2047), (9, 8200),
                (6, 16384), (3, 16392), (2, 65536), (1500, 256), (1100, 129)]
+# several rows per workgroup for every split of a row over threads
+LONG_SHAPES = [(70001, 24), (2100, 1030), (1030, 2050), (600, 5001), (520, 9000), (515, 17001)]
 STAT = 60 * R.U   # r: a chain of at most 64 squares per thread and 10 joins, halved by the root; few roundings more
 
 
@@ -374,6 +459,14 @@ def test_postnorm_and_gradient(T, h, following, gate, dtype):
     assert same_bits(dz2, dx)
     D.deamoe_postnorm(x, y, w, x, gate=gt, res_scale=a, eps=EPS)
     assert same_bits(x, z)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T,h", LONG_SHAPES)
+def test_norms_of_many_rows(T, h, dtype):
+    test_prenorm_and_gradient(T, h, dtype)
+    for gate, following in (("shared", True), ("full", False)):
+        test_postnorm_and_gradient(T, h, following, gate, dtype)
 
 
 def test_sums_over_no_tokens_are_zero():
@@ -473,6 +566,31 @@ def test_block_around_a_layer():
     D.deamoe_prenorm(x, w1, a)
     want = 0.5 * x.double() + gate.double() * (R.rms(layer(a).double(), EPS) * w2.double())
     close(z, want, 2 * STAT * (want.abs() + (0.5 * x.double()).abs() * 2 + 1e-30), F32, "z")
+
+
+def test_experts_and_blocks_on_a_given_stream():
+    """Everything that the classes launch runs on the stream given, and no token at all is a batch."""
+    g, s = gen(11), torch.cuda.Stream()
+    ex = experts(g, 12, 256, 160)
+    T = 400
+    x, ids, w = normal(g, T, 256, dtype=BF), ids_of(g, T, 3, 12, "topk"), torch.rand(T, 3, device="cuda", generator=g)
+    block = D.Block(lambda u, stream=None: ex(u, ids, w, stream=stream), *(normal(g, 256, dtype=BF) for _ in range(2)))
+    want, zwant = ex(x, ids, w), block(x)
+    late, y = torch.empty_like(x), torch.empty_like(x)
+    big = torch.randn(4096, 4096, device="cuda")
+    torch.cuda.synchronize()
+    for _ in range(3):
+        late.zero_()
+        torch.cuda.synchronize()
+        with torch.cuda.stream(s):
+            for _ in range(5):
+                big @ big            # x arrives late on this stream
+            late.copy_(x)
+        got = ex(late, ids, w, y=y, stream=s)
+        z = block(late, stream=s)
+        s.synchronize()
+        assert got is y and same_bits(got, want) and same_bits(z, zwant)
+    assert ex(x[:0], ids[:0], w[:0]).shape == (0, 256)
 
 
 def test_streams_and_repeats():

@@ -218,6 +218,20 @@ def test_binding_refuses_what_does_not_fit():
     _refused(D.deamoe_postnorm_backward, x, v, x, x, x, v.float(), gate=v, dgate=v)   # dgate is fp32
 
 
+def test_binding_refuses_missing_tensors():
+    i32, bf = torch.int32, torch.bfloat16
+    ids, x, off, pair = torch.zeros(4, 2, dtype=i32), torch.zeros(4, 8, dtype=bf), torch.zeros(9, dtype=i32), torch.zeros(8, dtype=i32)
+    xs, w, v = torch.zeros(8, 8, dtype=bf), torch.zeros(4, 2), torch.zeros(8, dtype=bf)
+    _refused(D.deamoe_dispatch, ids, None, off, pair, ids, xs)
+    _refused(D.deamoe_dispatch, ids, x, off, None, ids, xs)
+    _refused(D.deamoe_combine, ids, None, xs, x)
+    _refused(D.deamoe_combine_backward, ids, None, xs, x, xs, w)   # dys needs w
+    _refused(D.deamoe_combine_backward, ids, w, None, x, xs, w)    # dw needs ys
+    _refused(D.deamoe_prenorm, x, None, x)
+    _refused(D.deamoe_postnorm, x, None, v, x)
+    _refused(D.deamoe_postnorm_backward, x, v, None, x, x, v.float())
+
+
 def test_empty_batches_write_nothing_but_sums():
     """T = 0 with sums to clear is the only empty call that launches; the others return."""
     L = D.lib()
