@@ -226,11 +226,11 @@ __global__ __launch_bounds__(kThreads, 2) void w4_stream_kernel(W4Args a, int ks
     const int ntok = uniform(m1) - m0;
     const int r0 = uniform((int)(item % rt) * rows + (wv / ks) * NR * kTile);
     // The codes are read through buffer descriptors of the matrix's rows from r0
-    // on: a scalar offset moves with the step, each lane's offset stays, and
-    // rows past the last read as zeros (they are never stored).  A step that
-    // ends past the row's end reads the next row there, times an x of 0; a
-    // request past the last step goes to an empty buffer, which reads nothing,
-    // so that every iteration issues the same loads.
+    // on: base and size move with the step, each lane's offset stays, and rows
+    // past the last read as zeros (they are never stored).  A step that ends past
+    // the row's end reads the next row there, or past the last row zeros, times
+    // an x of 0; a request past the last step goes to an empty buffer, which reads
+    // nothing, so that every iteration issues the same loads.
     const uint32_t wrow = a.K / 2;
     char *wb[MATS];
     const void *sb[MATS];
@@ -249,14 +249,14 @@ __global__ __launch_bounds__(kThreads, 2) void w4_stream_kernel(W4Args a, int ks
         wo[n][i] = (n * kTile + i * 8 + (j & 7)) * wrow + ((j >> 3) * 4 + g) * 16;
     u32x4 W[D][NT][CH];
     auto request = [&](int q, int s) {
-      const int at = s < steps ? s * (SC / 2) : 0, bytes = s < steps ? (int)(left * wrow) : 0;
+      const int at = s < steps ? s * (SC / 2) : 0, bytes = s < steps ? (int)(left * wrow - at) : 0;
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
-        const auto buf = __builtin_amdgcn_make_buffer_rsrc(wb[n / NR], 0, bytes, 0x00027000);
+        const auto buf = __builtin_amdgcn_make_buffer_rsrc(wb[n / NR] + at, 0, bytes, 0x00027000);
 #pragma unroll
         for (int c = 0; c < CH; ++c)
           W[q][n][c] =
-              __builtin_amdgcn_raw_buffer_load_b128(buf, wo[n % NR][c & 1] + c / 2 * 128, at, KEEP ? 0 : kNonTemporal);
+              __builtin_amdgcn_raw_buffer_load_b128(buf, wo[n % NR][c & 1] + c / 2 * 128, 0, KEEP ? 0 : kNonTemporal);
       }
     };
 #pragma unroll
@@ -463,11 +463,11 @@ __global__ __launch_bounds__(kTileThreads, 2) void w4_tile_kernel(W4Args a) {
       xo[i] = (uint32_t)min(tid / 16 + i * (kTileThreads / 16), ntok - 1) * a.K * 2;
     u32x4 W[2][NT], X[XC];
     auto request_w = [&](int q, int s) {
-      const int bytes = s < steps ? (int)(left * wrow) : 0, at = s < steps ? s * (kTileStep / 2) : 0;
+      const int at = s < steps ? s * (kTileStep / 2) : 0, bytes = s < steps ? (int)(left * wrow - at) : 0;
 #pragma unroll
       for (int n = 0; n < NT; ++n)
         W[q][n] = __builtin_amdgcn_raw_buffer_load_b128(
-            __builtin_amdgcn_make_buffer_rsrc(wb[n / NR], 0, bytes, 0x00027000), wo[n % NR], at, 0);
+            __builtin_amdgcn_make_buffer_rsrc(wb[n / NR] + at, 0, bytes, 0x00027000), wo[n % NR], 0, 0);
     };
     auto request_x = [&](int s) {   // chunk tid % 16 of the step; past the row's end its first
       const uint32_t col = s * kTileStep + tid % 16 * 8, at = col < (uint32_t)a.K ? col * 2 : 0u;
