@@ -601,19 +601,29 @@ int64_t row_tiles(const W4Args &a, int rows) {
 
 dim3 grid_of(int64_t items) { return dim3((unsigned)(items < (1 << 20) ? items : 1 << 20)); }
 
-// K parts of a workgroup, at most `want`: a panel holds a round of the ring.
-int k_parts(const W4Args &a, int ntt, int want) {
+// K parts of the streaming kernel's workgroups, which there are `groups` of with
+// one part: as many as keep all workgroups on the CUs at once, of which each
+// holds three (two token tiles: two), and as a panel holds a round of the ring
+// for.  us, one | two | four parts: 4096 x 7168, one row, 64 workgroups of one
+// part, 20.5 | 13.5 | 9.7; 16384 x 7168, 256 of them, 22.0 | 16.9 | 21.8; 28672 x
+// 7168, 448 of them, 26.8 | 31.3 | 33.1; 8 rows of 8 experts of 2 x 2048 x 7168,
+// 256 of them, 31.8 | 27.7 | 34.9.
+int k_parts(const W4Args &a, int ntt, int64_t groups) {
   const int rows = a.M < kTile * ntt ? a.M : kTile * ntt, round = kRingColumns;
-  int ks = want;
-  while (ks > 1 && (ks * round > kPanelScales * a.group || ks * round > kPanelWords * ntt * 2 / rows - 8))
-    ks /= 2;
+  const int most = 256 * (ntt == 1 ? 3 : 2);
+  int ks = 1;
+  while (ks < kWaves && groups * ks * 2 <= most && ks * 2 * round <= kPanelScales * a.group &&
+         ks * 2 * round <= kPanelWords * ntt * 2 / rows - 8)
+    ks *= 2;
   return ks;
 }
 
 template <int MATS, int NR, int NTT, bool KEEP>
-hipError_t stream(const W4Args &a, int want, hipStream_t s) {
-  const int ks = k_parts(a, NTT, want), rows = kWaves / ks * NR * kTile;
-  const dim3 grid = grid_of(row_tiles(a, kTile * NTT) * ((a.R + rows - 1) / rows));
+hipError_t stream(const W4Args &a, hipStream_t s) {
+  const int64_t tiles = row_tiles(a, kTile * NTT);
+  const int most = kWaves * NR * kTile, ks = k_parts(a, NTT, tiles * ((a.R + most - 1) / most));
+  const int rows = most / ks;
+  const dim3 grid = grid_of(tiles * ((a.R + rows - 1) / rows));
   auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, s, a, ks); };
   if (a.group == 32) launch(w4_stream_kernel<MATS, NR, NTT, 1, KEEP>);
   else if (a.group == 64) launch(w4_stream_kernel<MATS, NR, NTT, 2, KEEP>);
@@ -642,22 +652,17 @@ hipError_t run(const W4Args &a, hipStream_t s) {
     // 1280, 44 | 43 at 12 rows, 65 | 56 at 24.
     const int64_t mean = a.M / a.n;
     if (mean > (MATS == 2 ? 28 : 14)) return tile<MATS>(a, s);
-    // Few workgroups: K over two waves (8 rows of 2 x 2048 x 7168: 31.7 -> 27.8 us).
-    // Many, of one matrix: four weight tiles per wave (82 experts of 4096 x 1536:
-    // 81 -> 75 us; but 48 of 2048 x 1280 34 -> 41).
-    const int64_t groups = row_tiles(a, kTile) * ((a.R + 63) / 64);
-    if (MATS == 1 && groups >= 5120) return stream<1, 4, 1, false>(a, 1, s);
-    return stream<MATS, 1, 1, false>(a, groups < 512 ? 2 : 1, s);
+    // Many workgroups, of one matrix: four weight tiles per wave (82 experts of
+    // 4096 x 1536: 81 -> 75 us; but 48 of 2048 x 1280 34 -> 41).
+    if (MATS == 1 && row_tiles(a, kTile) * ((a.R + 63) / 64) >= 5120) return stream<1, 4, 1, false>(a, s);
+    return stream<MATS, 1, 1, false>(a, s);
   }
   if ((int64_t)((a.M + 63) / 64) * blocks >= 256) return tile<MATS>(a, s);
-  // few tiles of a matrix: K over four waves, or two, so that all CUs take part
-  const int64_t tiles = (int64_t)((a.R + 15) / 16) * ((a.M + 15) / 16);
-  const int ks = tiles < 512 ? 4 : tiles < 704 ? 2 : 1;
-  if (a.M <= kTile) return stream<MATS, 1, 1, false>(a, ks, s);
+  if (a.M <= kTile) return stream<MATS, 1, 1, false>(a, s);
   // two token tiles per pass over the weights, us, one | two: 4096 x 4096, 22.8 |
   // 25.8 at 128 rows, 38.9 | 34.4 at 256; two matrices 53 | 64 at 200
-  if (MATS == 1 && a.M > 160) return stream<1, 1, 2, true>(a, ks, s);
-  return stream<MATS, 1, 1, true>(a, ks, s);
+  if (MATS == 1 && a.M > 160) return stream<1, 1, 2, true>(a, s);
+  return stream<MATS, 1, 1, true>(a, s);
 }
 
 }  // namespace
