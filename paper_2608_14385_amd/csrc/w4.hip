@@ -199,17 +199,25 @@ __device__ inline void rows_together(u32x4 &a, u32x4 &b) {
 // weights.  The scales of a panel's columns stand beside them, for each wave
 // its tiles': read by the lanes that need them, they would touch as many cache
 // lines as the weights.  Waves that share tiles add their sums over LDS at the
-// end.
+// end.  Every panel costs a round trip to the caches, so that WIDE panels take
+// all of a CU's LDS where a CU has one workgroup.
+// 82 of 128 experts of 2 x 1536 x 4096 for 16 tokens, 490 MB, take 93 us: 5.3 TB/s,
+// bound by HBM.  7168 x 7168 for one row takes 11 us, of which the weights'
+// 27 MB need 5.5.
 constexpr int kPanelWords = 16 * (1024 + 8) / 2;   // of a token tile, 4 bytes each
 constexpr int kPanelScales = 32;                   // of a weight row, at most
+constexpr int kWidePanel = 4;                      // token tiles' words in a wide panel
+// wide: 16 token rows of 4096 columns and the scales, 149 of 160 KB
+constexpr int panel_words(int ntt, bool wide) { return kPanelWords * (wide ? kWidePanel : ntt); }
+constexpr int panel_scales(int tiles, bool wide) { return wide ? 64 / tiles : kPanelScales; }
 constexpr int kNonTemporal = 2;                    // cache policy of a buffer load
 constexpr int kRingColumns = 512;                  // two steps of 256: a round of the ring
-template <int MATS, int NR, int NTT, int G32, bool KEEP>
+template <int MATS, int NR, int NTT, int G32, bool KEEP, bool WIDE>
 __global__ __launch_bounds__(kThreads, 2) void w4_stream_kernel(W4Args a, int ks) {
   constexpr int D = 2, CH = 2, SC = 128 * CH, NT = MATS * NR, GS = 32 * G32;
-  constexpr int TR = NTT * kTile, WORDS = kPanelWords * NTT;
+  constexpr int TR = NTT * kTile, WORDS = panel_words(NTT, WIDE), SCALES = panel_scales(NT, WIDE);
   __shared__ __align__(16) uint32_t s_x[WORDS];
-  __shared__ float s_scale[kWaves][NT][kTile][kPanelScales + 1];
+  __shared__ float s_scale[kWaves][NT][kTile][SCALES + 1];
   static_assert(kWaves * NT * NTT * 4 * kWave <= WORDS, "the sums of the waves");
   static_assert(CH % 2 == 0, "steps of whole cache lines");
   static_assert(D * SC == kRingColumns && kRingColumns <= 1024, "a panel holds a round of the ring");
@@ -264,7 +272,7 @@ __global__ __launch_bounds__(kThreads, 2) void w4_stream_kernel(W4Args a, int ks
 
     // panels: whole rounds of all ring places of all K parts
     const int round = D * ks * SC, prow = min(ntok, TR);
-    const int pcol = min(min(WORDS * 2 / prow - 8, a.K + round - 1), kPanelScales * GS) / round * round;
+    const int pcol = min(min(WORDS * 2 / prow - 8, a.K + round - 1), SCALES * GS) / round * round;
     const int ldx = pcol + 8;
     uint32_t xo[NTT];
 #pragma unroll
@@ -315,21 +323,21 @@ __global__ __launch_bounds__(kThreads, 2) void w4_stream_kernel(W4Args a, int ks
     for (int p0 = 0; p0 < a.K; p0 += pcol) {
       __syncthreads();   // the last panel, or the last item's sums, have been read
       const int q0 = p0 / GS, nq = min(groups - q0, pcol / GS);
-      // this wave's scales, two rows at a time; past the end the sums are 0, and
+      // this wave's scales; past the end the sums are 0, and
       // their scale is
-      constexpr int N = kTile * kPanelScales / kWave;
-      const int sr = lane / kPanelScales, sq = lane % kPanelScales;
+      constexpr int N = kTile * SCALES / kWave;
+      const int sr = lane / SCALES, sq = lane % SCALES;
       uint32_t sv[NT][N];
 #pragma unroll
       for (int n = 0; n < NT; ++n)
         with_scales(sb[n / NR], a.scale_bf16, [&](auto *from, int) {
 #pragma unroll
           for (int i = 0; i < N; ++i) {
-            const int r = (n % NR) * kTile + i * 2 + sr;
+            const int r = (n % NR) * kTile + i * (kWave / SCALES) + sr;
             sv[n][i] = from[sq < nq && r < left ? r * groups + q0 + sq : 0];
           }
         });
-      constexpr int U = NTT == 1 ? 8 : 16;   // 16-byte chunks of x in flight
+      constexpr int U = NTT == 1 && !WIDE ? 8 : 16;   // 16-byte chunks of x in flight
       const int chunks = pcol / 8, total = prow * chunks;
       // i / chunks = i * inverse / 2^32: both are below 2^15, so that the
       // inverse's excess times i stays below 2^32
@@ -357,8 +365,8 @@ __global__ __launch_bounds__(kThreads, 2) void w4_stream_kernel(W4Args a, int ks
       for (int n = 0; n < NT; ++n)
 #pragma unroll
         for (int i = 0; i < N; ++i)
-          s_scale[wv][n][i * 2 + sr][sq] =
-              sq < nq && (n % NR) * kTile + i * 2 + sr < left
+          s_scale[wv][n][i * (kWave / SCALES) + sr][sq] =
+              sq < nq && (n % NR) * kTile + i * (kWave / SCALES) + sr < left
                   ? __uint_as_float(sv[n][i] << (a.scale_bf16 ? 16 : 0)) : 0.f;
       __syncthreads();
       const int end = min(p0 + pcol, a.K);
@@ -417,6 +425,12 @@ __global__ __launch_bounds__(kThreads, 2) void w4_stream_kernel(W4Args a, int ks
 // Both operands of the next step are requested before a step's products; the
 // token rows go through registers, where they take the codes' order, into the
 // other half of the LDS buffer.
+// 8192 rows through 2048 x 8192 run at 840 TFLOP/s; 12288 rows through 64 experts
+// of 2 x 1280 x 2048, whose tiles are a quarter empty and whose sums are short, in
+// 209 us, 616 TFLOP/s.  A step's 32 KB for 4 MFLOP keep a CU's loads at 19 bytes
+// per ns, near the 21 of a stream from HBM on all CUs, and unpacking takes about
+// half as many issue cycles as the products; more steps in flight, 128-row tiles
+// and pairs of steps were no faster.
 constexpr int kTileTok = 64, kTileStep = 128, kTileStride = kTileStep + 8;
 constexpr int kTileThreads = 256, kTileWaves = kTileThreads / kWave, kTileWeights = 4;
 template <int MATS, int G32>
@@ -608,27 +622,45 @@ dim3 grid_of(int64_t items) { return dim3((unsigned)(items < (1 << 20) ? items :
 // part, 20.5 | 13.5 | 9.7; 16384 x 7168, 256 of them, 22.0 | 16.9 | 21.8; 28672 x
 // 7168, 448 of them, 26.8 | 31.3 | 33.1; 8 rows of 8 experts of 2 x 2048 x 7168,
 // 256 of them, 31.8 | 27.7 | 34.9.
-int k_parts(const W4Args &a, int ntt, int64_t groups) {
-  const int rows = a.M < kTile * ntt ? a.M : kTile * ntt, round = kRingColumns;
-  const int most = 256 * (ntt == 1 ? 3 : 2);
+struct Parts {
+  int ks, columns;   // K parts, columns of a panel
+};
+Parts k_parts(const W4Args &a, int ntt, int64_t groups, int most, int words, int scales) {
+  const int rows = a.M < kTile * ntt ? a.M : kTile * ntt, in_x = words * 2 / rows - 8;
+  const int columns = in_x < scales * a.group ? in_x : scales * a.group;
   int ks = 1;
-  while (ks < kWaves && groups * ks * 2 <= most && ks * 2 * round <= kPanelScales * a.group &&
-         ks * 2 * round <= kPanelWords * ntt * 2 / rows - 8)
-    ks *= 2;
-  return ks;
+  while (ks < kWaves && groups * ks * 2 <= most && ks * 2 * kRingColumns <= columns) ks *= 2;
+  return {ks, columns / (ks * kRingColumns) * (ks * kRingColumns)};
+}
+
+template <int MATS, int NR, int NTT, bool KEEP, bool WIDE>
+hipError_t stream_panels(const W4Args &a, int64_t tiles, int ks, hipStream_t s) {
+  const int rows = kWaves / ks * NR * kTile;
+  const dim3 grid = grid_of(tiles * ((a.R + rows - 1) / rows));
+  auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, s, a, ks); };
+  if (a.group == 32) launch(w4_stream_kernel<MATS, NR, NTT, 1, KEEP, WIDE>);
+  else if (a.group == 64) launch(w4_stream_kernel<MATS, NR, NTT, 2, KEEP, WIDE>);
+  else launch(w4_stream_kernel<MATS, NR, NTT, 4, KEEP, WIDE>);
+  return hipGetLastError();
 }
 
 template <int MATS, int NR, int NTT, bool KEEP>
 hipError_t stream(const W4Args &a, hipStream_t s) {
+  constexpr int kCus = 256;
   const int64_t tiles = row_tiles(a, kTile * NTT);
-  const int most = kWaves * NR * kTile, ks = k_parts(a, NTT, tiles * ((a.R + most - 1) / most));
-  const int rows = most / ks;
-  const dim3 grid = grid_of(tiles * ((a.R + rows - 1) / rows));
-  auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, s, a, ks); };
-  if (a.group == 32) launch(w4_stream_kernel<MATS, NR, NTT, 1, KEEP>);
-  else if (a.group == 64) launch(w4_stream_kernel<MATS, NR, NTT, 2, KEEP>);
-  else launch(w4_stream_kernel<MATS, NR, NTT, 4, KEEP>);
-  return hipGetLastError();
+  const int64_t groups = tiles * ((a.R + kWaves * NR * kTile - 1) / (kWaves * NR * kTile));
+  const Parts p = k_parts(a, NTT, groups, kCus * (NTT == 1 ? 3 : 2), panel_words(NTT, false), kPanelScales);
+  if constexpr (NR == 1 && NTT == 1) {
+    // With no more workgroups than CUs, panels that fill a CU's LDS, where they
+    // allow more parts or are four times as wide; us, narrow | wide: 4096 x 7168,
+    // 16 rows, 22.9 | 18.2, two matrices of 4096 x 4096 19.7 | 12.8; with as many
+    // parts of panels twice as wide, 7168 x 7168 in groups of 32, 22.7 | 25.9.
+    const Parts w = k_parts(a, NTT, groups, kCus, panel_words(NTT, true), panel_scales(MATS, true));
+    if (groups * w.ks <= kCus && p.columns < a.K &&
+        (w.ks > p.ks || (w.ks == p.ks && w.columns >= 4 * p.columns)))
+      return stream_panels<MATS, NR, NTT, KEEP, true>(a, tiles, w.ks, s);
+  }
+  return stream_panels<MATS, NR, NTT, KEEP, false>(a, tiles, p.ks, s);
 }
 
 template <int MATS>

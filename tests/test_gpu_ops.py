@@ -250,6 +250,7 @@ def test_w4_experts(T, k, n, R_, K, group, kind):
     (2048, 2050, 1152, 128), (1100, 4000, 320, 64), (1030, 4097, 2080, 32),   # 64-row tiles
     (160, 700, 2112, 64), (161, 1500, 4128, 32), (250, 2100, 1152, 128),      # one and two token tiles
     (16, 8300, 1056, 32), (12, 10000, 192, 64), (9, 12001, 4224, 128),        # K over four, two waves, one
+    (16, 700, 7200, 32), (9, 300, 4288, 64), (30, 500, 7296, 128), (3, 260, 16544, 32), (5, 33, 9088, 64),   # wide panels
 ])
 def test_w4_linear_by_kernel(M, R_, K, group, scale):
     """Sizes on either side of what chooses the kernel and its split, with a K that ends inside a step
