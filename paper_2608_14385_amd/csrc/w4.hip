@@ -426,11 +426,11 @@ __global__ __launch_bounds__(kThreads, 2) void w4_stream_kernel(W4Args a, int ks
 // token rows go through registers, where they take the codes' order, into the
 // other half of the LDS buffer.
 // 8192 rows through 2048 x 8192 run at 840 TFLOP/s; 12288 rows through 64 experts
-// of 2 x 1280 x 2048, whose tiles are a quarter empty and whose sums are short, in
+// of 2 x 1280 x 2048, whose tiles are a seventh empty and whose sums are short, in
 // 209 us, 616 TFLOP/s.  A step's 32 KB for 4 MFLOP keep a CU's loads at 19 bytes
 // per ns, near the 21 of a stream from HBM on all CUs, and unpacking takes about
-// half as many issue cycles as the products; more steps in flight, 128-row tiles
-// and pairs of steps were no faster.
+// half as many issue cycles as the products; more steps in flight, wider
+// workgroups and pairs of steps were no faster.
 constexpr int kTileTok = 64, kTileStep = 128, kTileStride = kTileStep + 8;
 constexpr int kTileThreads = 256, kTileWaves = kTileThreads / kWave, kTileWeights = 4;
 template <int MATS, int G32>
