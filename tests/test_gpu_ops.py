@@ -126,6 +126,22 @@ def test_dispatch_rows_past_four_gigabytes():
     close(y[-500:], want, 9 * R.U * want.abs(), BF, "combine")
 
 
+def test_dispatch_of_the_most_pairs():
+    T, k, n = 1 << 23, 8, 64
+    say(f"[gpu] dispatch of {T * k} pairs")
+    g = gen(2)
+    ids, x = ids_of(g, T, k, n, "any"), normal(g, T, 1, dtype=BF)
+    s = Sorted(ids, n, x)
+    key, pair = torch.sort(ids.flatten(), stable=True)
+    assert torch.equal(s.pair, pair.to(I32))
+    assert torch.equal(s.row.flatten()[pair], torch.arange(T * k, dtype=I32, device="cuda"))
+    assert torch.equal(s.offset, torch.searchsorted(key, torch.arange(n + 1, dtype=I32, device="cuda")).to(I32))
+    assert torch.equal(s.xs, x[pair // k])
+    dx = torch.empty_like(x)
+    D.deamoe_dispatch_backward(s.row, s.xs, dx)
+    assert torch.equal(dx, 8 * x)   # eight times the same, exactly
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("T,k,n,h,kind", [
     (1, 1, 1, 1, "any"), (1, 10, 672, 1024, "topk"), (7, 32, 64, 7, "stray"), (61, 8, 256, 7168, "topk"),
@@ -468,6 +484,18 @@ def test_norms_of_many_rows(T, h, dtype):
     test_prenorm_and_gradient(T, h, dtype)
     for gate, following in (("shared", True), ("full", False)):
         test_postnorm_and_gradient(T, h, following, gate, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T,h", [(7, 129), (3, 7168), (2, 16392), (2, 65536)])
+def test_postnorm_in_place_with_the_next_norm(T, h, dtype):
+    g, t = gen(h), TYPES[dtype]
+    x, y, gate = (normal(g, T, h, dtype=t) for _ in range(3))
+    w, wn = normal(g, h, dtype=t), normal(g, h, dtype=t)
+    z, u, v = (torch.empty_like(x) for _ in range(3))
+    D.deamoe_postnorm(x, y, w, z, gate=gate, w_next=wn, u=u)
+    D.deamoe_postnorm(x, y, w, x, gate=gate, w_next=wn, u=v)
+    assert same_bits(x, z) and same_bits(u, v)
 
 
 def test_sums_over_no_tokens_are_zero():
