@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import contextlib
 import ctypes as C
+import functools
 import os
 from dataclasses import dataclass
 
@@ -349,6 +350,7 @@ def _rows(what: str, t: torch.Tensor, name: str) -> tuple:
     return t.shape
 
 
+@functools.lru_cache(maxsize=1024)   # of sizes alone; 10 pairs sorted in 8.5 us, not 8.9
 def deamoe_dispatch_workspace_bytes(T: int, k: int, n: int) -> int:
     return _bytes(lib().deamoe_dispatch_workspace_bytes, T, k, n)
 
@@ -444,6 +446,7 @@ def deamoe_w4_swiglu(x, gate_codes, gate_scale, up_codes, up_scale, y, offset=No
          y.data_ptr())
 
 
+@functools.lru_cache(maxsize=1024)
 def deamoe_norm_workspace_bytes(T: int, h: int) -> int:
     return _bytes(lib().deamoe_norm_workspace_bytes, T, h)
 
