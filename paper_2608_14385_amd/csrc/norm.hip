@@ -39,6 +39,7 @@ __device__ inline float lane_value(float v, int lane) {
 // reductions in a row use different halves of `s`, so that one barrier each is
 // enough.
 constexpr int kMaxWaves = 16, kMaxSums = 3;
+constexpr int kRowWaves = 4;   // rows at a time in the gradients of rows of one wave
 struct Reduce {
   float (*s)[kMaxSums][kMaxWaves];
   int flip = 0;
@@ -177,7 +178,8 @@ __global__ __launch_bounds__(MAXG) void postnorm_kernel(PostnormArgs a) {
 // Gradients.  MODE: the norm before a block alone, the one after it alone, or
 // the one after it with the next one before.  A workgroup walks over rows t,
 // t + grid, ... and keeps its sums over them for its columns: in registers, or
-// for wide rows in its part of the workspace.  8192 rows of 4096 in bf16 with both
+// for wide rows in its part of the workspace.  Rows that one wave holds are taken
+// four at a time, a wave each (blockDim.y), whose sums are joined in LDS.  8192 rows of 4096 in bf16 with both
 // norms and a shared gate, 403 MB, take 89 us: 4.5 TB/s, of a copy's 4.9.
 enum NormMode : int { NORM_PRE = 0, NORM_POST = 1, NORM_BOTH = 2 };
 
@@ -198,6 +200,9 @@ __global__ __launch_bounds__(MAXG) void norm_backward_kernel(NormBackwardArgs a)
   Reduce red{s_red};
   const int h = a.h;
   float *part = a.part + (size_t)blockIdx.x * 3 * h;   // dw, dw_next, dgate
+  constexpr bool ROWS = N == 1 && MAXG == 256;   // several rows at a time; the row stays a scalar
+  const int y = ROWS ? __builtin_amdgcn_readfirstlane(threadIdx.y) : 0, ny = ROWS ? blockDim.y : 1;
+  const int t0 = blockIdx.x * ny + y, step = gridDim.x * ny;
   float sum[3][NH][V] = {};
   auto add = [&](int which, int i, int c, bool first, const float (&v)[V]) {
     if constexpr (N > 0) {
@@ -213,14 +218,14 @@ __global__ __launch_bounds__(MAXG) void norm_backward_kernel(NormBackwardArgs a)
   };
   const Row<F32, POST ? N : 0> w(a.w, 0, h);
   const Row<F32, NEXT ? N : 0> w_next(a.w_next, 0, h);
-  BackwardRows<F32, N, MODE> next(a, blockIdx.x);
-  for (int t = blockIdx.x; t < a.T; t += gridDim.x) {
-    const bool first = t == (int)blockIdx.x;
+  BackwardRows<F32, N, MODE> next(a, min(t0, a.T - 1));
+  for (int t = t0; t < a.T; t += step) {
+    const bool first = t == t0;
     const BackwardRows<F32, N, MODE> r = next;
     const Row<F32, POST ? N : 0> gate(a.gate_mode == DEAMOE_GATE_NONE ? a.w : a.gate,
                                       a.gate_mode == DEAMOE_GATE_FULL ? t : 0, h);
     // the next row is on its way while this one waits for its sums
-    if (t + (int)gridDim.x < a.T) next = BackwardRows<F32, N, MODE>(a, t + gridDim.x);
+    if (t + step < a.T) next = BackwardRows<F32, N, MODE>(a, t + step);
     float s1[3] = {0.f, 0.f, 0.f};   // z^2, du w' z, y^2
     chunks<F32, N>(h, [&](int i, int c) {
       if constexpr (NEXT) {
@@ -314,6 +319,22 @@ __global__ __launch_bounds__(MAXG) void norm_backward_kernel(NormBackwardArgs a)
       store_chunk<F32>(row_at<F32>(a.dx, t, h), c, h, pack_chunk<F32>(d));
     });
   }
+  if constexpr (ROWS)
+    if (ny > 1) {
+      __shared__ float s_sum[kRowWaves - 1][3][V][kWave];
+      if (y)
+#pragma unroll
+        for (int which = 0; which < 3; ++which)
+#pragma unroll
+          for (int e = 0; e < V; ++e) s_sum[y - 1][which][e][threadIdx.x] = sum[which][0][e];
+      __syncthreads();
+      if (y) return;
+      for (int o = 0; o < kRowWaves - 1; ++o)
+#pragma unroll
+        for (int which = 0; which < 3; ++which)
+#pragma unroll
+          for (int e = 0; e < V; ++e) sum[which][0][e] += s_sum[o][which][e][threadIdx.x];
+    }
   if constexpr (N > 0)
     chunks<F32, N>(h, [&](int i, int c) {
 #pragma unroll
@@ -328,34 +349,32 @@ __global__ __launch_bounds__(MAXG) void norm_backward_kernel(NormBackwardArgs a)
     });
 }
 
-// out[c] = sum over the workgroups' parts.  A workgroup takes 64 columns; its 16
-// waves take every 16th part, eight loads in flight, and are joined in order.
+// out[c] = sum over the workgroups' parts.  A workgroup takes COLS columns; its
+// 1024 / COLS runs of lanes take a part in turn, 8 loads in flight, and are
+// joined in order.
 struct ColumnSumArgs {
   const float *part[3];     // stride of the parts: 3 * h
   float *out[3];
   int32_t h, blocks;
 };
+template <int COLS>
 __global__ __launch_bounds__(1024) void column_sum_kernel(ColumnSumArgs a) {
-  constexpr int W = 16, U = 8;
-  __shared__ float s_sum[W][kWave];
-  const int lane = threadIdx.x % kWave, wv = threadIdx.x / kWave;
-  const int c = blockIdx.x * kWave + lane;
+  constexpr int W = 1024 / COLS, U = 8;
+  __shared__ float s_sum[W][COLS];
+  const int lane = threadIdx.x % COLS, at = threadIdx.x / COLS;
+  const int c = blockIdx.x * COLS + lane;
   const float *p = a.part[blockIdx.y] + min(c, a.h - 1);
   float v = 0.f;
-  for (int b0 = wv; b0 < a.blocks; b0 += W * U) {
+  for (int b0 = at; b0 < a.blocks; b0 += W * U) {
     float t[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int b = b0 + u * W;
-      t[u] = p[(size_t)min(b, a.blocks - 1) * 3 * a.h];
-      t[u] = b < a.blocks ? t[u] : 0.f;
-    }
+    for (int u = 0; u < U; ++u) t[u] = p[(size_t)min(b0 + u * W, a.blocks - 1) * 3 * a.h];
 #pragma unroll
-    for (int u = 0; u < U; ++u) v += t[u];
+    for (int u = 0; u < U; ++u) v += b0 + u * W < a.blocks ? t[u] : 0.f;
   }
-  s_sum[wv][lane] = v;
+  s_sum[at][lane] = v;
   __syncthreads();
-  if (wv == 0 && c < a.h) {
+  if (at == 0 && c < a.h) {
     float total = 0.f;
 #pragma unroll
     for (int i = 0; i < W; ++i) total += s_sum[i][lane];
@@ -386,16 +405,16 @@ Shape shape_of(int h, int act_f32) {
 constexpr int kRowGrid = 1 << 16;   // workgroups at most; further rows are walked to
 
 template <bool F32, int N, int MAXG>
-hipError_t backward_shaped(const NormBackwardArgs &a, int threads, int blocks, hipStream_t s) {
+hipError_t backward_shaped(const NormBackwardArgs &a, dim3 threads, int blocks, hipStream_t s) {
   if (!a.y)
-    hipLaunchKernelGGL((norm_backward_kernel<F32, N, MAXG, NORM_PRE>), dim3(blocks), dim3(threads),
-                       0, s, a);
+    hipLaunchKernelGGL((norm_backward_kernel<F32, N, MAXG, NORM_PRE>), dim3(blocks), threads, 0,
+                       s, a);
   else if (a.du)
     hipLaunchKernelGGL((norm_backward_kernel<F32, N, MAXG, NORM_BOTH>), dim3(blocks),
-                       dim3(threads), 0, s, a);
+                       threads, 0, s, a);
   else
     hipLaunchKernelGGL((norm_backward_kernel<F32, N, MAXG, NORM_POST>), dim3(blocks),
-                       dim3(threads), 0, s, a);
+                       threads, 0, s, a);
   return hipGetLastError();
 }
 
@@ -417,15 +436,18 @@ hipError_t with_shape(Shape sh, bool f32, F f) {
 
 }  // namespace
 
-// As many workgroups as run at once (eight waves on each of the 256 CUs; one
-// workgroup at least; 1024 at most, whose parts are summed afterwards), and of
-// those as many as share the rows evenly.
-int norm_backward_blocks(int T, int h) {
-  const int threads = shape_of(h, 0).threads;   // the smaller of the two types' shapes
+// As many workgroups as run at once (eight waves on each of the 256 CUs, sixteen
+// of rows of one wave; one workgroup at least; 1024 at most, whose parts are
+// summed afterwards), and of those as many as share the rows evenly.  Four rows
+// at a time: pre-norm and gradient of 16384 rows of 256 in 24.7 us, one at a time
+// 40.5.
+int norm_backward_blocks(int T, int h, int act_f32) {
+  const int threads = shape_of(h, act_f32).threads;
   const int most = threads >= 512 ? 256 : threads >= 128 ? 131072 / threads : 1024;
-  if (T <= most) return T;
-  const int rows = (T + most - 1) / most;
-  return (T + rows - 1) / rows;
+  const int at_once = threads == kWave ? kRowWaves : 1, groups = (T + at_once - 1) / at_once;
+  if (groups <= most) return groups;
+  const int rows = (groups + most - 1) / most;
+  return (groups + rows - 1) / rows;
 }
 
 hipError_t launch_prenorm(const PrenormArgs &a, hipStream_t s) {
@@ -448,9 +470,10 @@ hipError_t launch_postnorm(const PostnormArgs &a, hipStream_t s) {
 
 hipError_t launch_norm_backward(const NormBackwardArgs &a, hipStream_t s) {
   const Shape sh = shape_of(a.h, a.act_f32);
-  const int blocks = norm_backward_blocks(a.T, a.h);
+  const int blocks = norm_backward_blocks(a.T, a.h, a.act_f32);
   const hipError_t e = with_shape(sh, a.act_f32, [&](auto F32, auto N, auto G) {
-    return backward_shaped<F32.value, N.value, G.value>(a, sh.threads, blocks, s);
+    return backward_shaped<F32.value, N.value, G.value>(
+        a, dim3(sh.threads, sh.threads == kWave ? kRowWaves : 1), blocks, s);
   });
   if (e != hipSuccess) return e;
   ColumnSumArgs c;
@@ -464,7 +487,11 @@ hipError_t launch_norm_backward(const NormBackwardArgs &a, hipStream_t s) {
   if (a.gate_mode == DEAMOE_GATE_SHARED) sum_of(2, a.dgate);
   c.h = a.h;
   c.blocks = blocks;
-  hipLaunchKernelGGL(column_sum_kernel, dim3((a.h + kWave - 1) / kWave, n), dim3(1024), 0, s, c);
+  // Few columns: half a wave of them each, for twice the workgroups.  us of the
+  // whole gradient, 64 | 32 columns: 8192 rows of 1024, 30 | 28; 64 of 7168, 16.5 |
+  // 17.1.
+  if (a.h <= 2048) hipLaunchKernelGGL(column_sum_kernel<32>, dim3((a.h + 31) / 32, n), dim3(1024), 0, s, c);
+  else hipLaunchKernelGGL(column_sum_kernel<64>, dim3((a.h + 63) / 64, n), dim3(1024), 0, s, c);
   return hipGetLastError();
 }
 

@@ -166,7 +166,7 @@ struct NormBackwardArgs {
   float *dw, *dw_next;
   float *part;              // workspace: [blocks, 3, h]
 };
-int norm_backward_blocks(int T, int h);
+int norm_backward_blocks(int T, int h, int act_f32);
 hipError_t launch_prenorm(const PrenormArgs &a, hipStream_t s);
 hipError_t launch_postnorm(const PostnormArgs &a, hipStream_t s);
 hipError_t launch_norm_backward(const NormBackwardArgs &a, hipStream_t s);

@@ -210,8 +210,9 @@ int deamoe_postnorm(int32_t T, int32_t h, int32_t act_dtype, float eps, float re
   return check(launch_postnorm(a, static_cast<hipStream_t>(stream)));
 }
 
-static size_t norm_bytes(int32_t T, int32_t h) {
-  return align16((size_t)norm_backward_blocks(T, h) * 3 * h * 4);
+static size_t norm_bytes(int32_t T, int32_t h) {   // enough for either type
+  const int bf16 = norm_backward_blocks(T, h, 0), f32 = norm_backward_blocks(T, h, 1);
+  return align16((size_t)(bf16 > f32 ? bf16 : f32) * 3 * h * 4);
 }
 
 int deamoe_norm_workspace_bytes(int32_t T, int32_t h, size_t *bytes) {
