@@ -201,7 +201,7 @@ __device__ inline void rows_together(u32x4 &a, u32x4 &b) {
 // lines as the weights.  Waves that share tiles add their sums over LDS at the
 // end.  Every panel costs a round trip to the caches, so that WIDE panels take
 // all of a CU's LDS where a CU has one workgroup.
-// 82 of 128 experts of 2 x 1536 x 4096 for 16 tokens, 490 MB, take 93 us: 5.3 TB/s,
+// 82 of 128 experts of 2 x 1536 x 4096 for 16 tokens, 490 MB, take 90 us: 5.5 TB/s,
 // bound by HBM.  7168 x 7168 for one row takes 11 us, of which the weights'
 // 27 MB need 5.5.
 constexpr int kPanelWords = 16 * (1024 + 8) / 2;   // of a token tile, 4 bytes each
