@@ -311,6 +311,15 @@ def _act(what: str, t: torch.Tensor) -> int:
     raise DeamoeError(ERR_INVALID, f"{what}: {t.dtype} is neither bfloat16 nor float32")
 
 
+def _on(dev: int, stream):
+    """A context in which device `dev` is the current one and, where one is given, `stream` its current stream."""
+    if stream is not None:
+        return torch.cuda.stream(stream)
+    if dev >= 0 and dev != torch.cuda.current_device():
+        return torch.cuda.device(dev)
+    return contextlib.nullcontext()
+
+
 def _call(fn, dev: int, stream, args) -> int:
     """fn(*args, stream) with device `dev` current; the stream is its current one unless given."""
     if dev < 0:
@@ -330,7 +339,7 @@ def _run_with_workspace(fn, dev: int, stream, ws, nbytes: int, *args):
     """The same for a call whose last two arguments are its workspace: the given one, or one of torch's
     for the stream that the call runs on."""
     if ws is None and nbytes and dev >= 0:
-        with contextlib.nullcontext() if stream is None else torch.cuda.stream(stream):
+        with contextlib.nullcontext() if stream is None else _on(dev, stream):
             ws = torch.empty(nbytes, dtype=torch.uint8, device=torch.device("cuda", dev))
     elif ws is not None and (ws.get_device() != dev or not ws.is_contiguous()):
         raise DeamoeError(ERR_WORKSPACE, f"{fn.__name__}: workspace is not contiguous, or not on device {dev}")
@@ -537,7 +546,7 @@ class W4Experts:
     def __call__(self, x, topk_ids, topk_w, y=None, stream=None):
         """y [T, h] from x [T, h] (bf16), topk_ids [T, k] (int32, -1: none) and topk_w [T, k] (fp32)."""
         if stream is not None:
-            with torch.cuda.stream(stream):
+            with _on(x.get_device(), stream):
                 return self(x, topk_ids, topk_w, y)
         T, k = topk_ids.shape
         new, i32 = dict(device=x.device), torch.int32
@@ -563,15 +572,14 @@ class Block:
 
     def __call__(self, x, u=None, stream=None, **kw):
         """z, or with w_next (z, u): u is the next block's normed input, which its call takes in
-        place of norming x again.  Further keyword arguments go to the layer."""
-        if stream is not None:
-            with torch.cuda.stream(stream):
-                return self(x, u, **kw)
-        if u is None:
-            u = torch.empty_like(x)
-            deamoe_prenorm(x, self.w_pre, u, eps=self.eps)
-        y, z = self.layer(u, **kw), torch.empty_like(x)
-        nxt = torch.empty_like(x) if self.w_next is not None else None
-        deamoe_postnorm(x, y, self.w_post, z, gate=self.gate, res_scale=self.res_scale,
-                        w_next=self.w_next, u=nxt, eps=self.eps)
-        return z if nxt is None else (z, nxt)
+        place of norming x again.  Further keyword arguments go to the layer, which runs with x's
+        device and the call's stream as the current ones."""
+        with _on(x.get_device(), stream):
+            if u is None:
+                u = torch.empty_like(x)
+                deamoe_prenorm(x, self.w_pre, u, eps=self.eps)
+            y, z = self.layer(u, **kw), torch.empty_like(x)
+            nxt = torch.empty_like(x) if self.w_next is not None else None
+            deamoe_postnorm(x, y, self.w_post, z, gate=self.gate, res_scale=self.res_scale,
+                            w_next=self.w_next, u=nxt, eps=self.eps)
+            return z if nxt is None else (z, nxt)

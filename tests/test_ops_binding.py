@@ -1,0 +1,75 @@
+"""The binding of the operators beside the layer, on the CPU: which device and stream a call runs on."""
+import contextlib
+import os
+import sys
+
+import pytest
+import torch
+
+sys.path.insert(0, os.path.dirname(os.path.abspath(__file__)))
+from paper_2608_14385_amd import deamoe as D  # noqa: E402
+
+
+class OnSecond(torch.Tensor):
+    """A CPU tensor that says it is on the second GPU."""
+
+    def get_device(self):
+        return 1
+
+
+class Stream:
+    def __init__(self, index, handle):
+        self.device, self.cuda_stream = torch.device("cuda", index), handle
+
+
+@pytest.fixture
+def gpus(monkeypatch):
+    """Two GPUs, the first of them current; yields a function that says what is current."""
+    state = {"device": 0, 0: "default 0", 1: "default 1"}
+
+    @contextlib.contextmanager
+    def device(index):
+        before, state["device"] = state["device"], index
+        yield
+        state["device"] = before
+
+    @contextlib.contextmanager
+    def stream(s):
+        i = s.device.index
+        before, state[i] = state[i], s.cuda_stream
+        with device(i):
+            yield
+        state[i] = before
+
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: state["device"])
+    monkeypatch.setattr(torch.cuda, "device", device)
+    monkeypatch.setattr(torch.cuda, "stream", stream)
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda i: state[i], raising=False)
+    return lambda: (state["device"], state[state["device"]])
+
+
+@pytest.mark.parametrize("stream", [None, Stream(1, "side")])
+def test_a_blocks_layer_runs_where_its_rows_are(gpus, monkeypatch, stream):
+    """Norms and layer run on the same device and stream, that of x and the call, also where another
+    device is the current one."""
+    ran = []
+    monkeypatch.setattr(D, "_run", lambda fn, dev, stream, *args: ran.append(("norm", dev, gpus())))
+
+    def layer(u):
+        ran.append(("layer", u.get_device(), gpus()))
+        return u
+
+    x, w = (torch.zeros(*s).as_subclass(OnSecond) for s in ((4, 8), (8,)))
+    D.Block(layer, w, w)(x, stream=stream)
+    here = (1, "default 1" if stream is None else "side")
+    assert ran == [("norm", 1, here), ("layer", 1, here), ("norm", 1, here)]
+    assert gpus() == (0, "default 0")
+
+
+def test_a_call_runs_on_its_tensors_device(gpus):
+    def fn(*args):
+        return args, gpus()
+
+    assert D._call(fn, 1, None, (7,)) == ((7, "default 1"), (1, "default 1"))
+    assert D._call(fn, 1, Stream(1, "side"), (7,))[0] == (7, "side")
+    assert D._call(fn, 0, None, (7,)) == ((7, "default 0"), (0, "default 0"))
