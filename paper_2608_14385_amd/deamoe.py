@@ -311,9 +311,15 @@ def _act(what: str, t: torch.Tensor) -> int:
     raise DeamoeError(ERR_INVALID, f"{what}: {t.dtype} is neither bfloat16 nor float32")
 
 
-def _on(dev: int, stream):
+def _same_device(what: str, dev: int, stream):
+    if stream.device.index != dev:
+        raise DeamoeError(ERR_INVALID, f"{what}: the stream is on {stream.device}, the tensors are on device {dev}")
+
+
+def _on(what: str, dev: int, stream):
     """A context in which device `dev` is the current one and, where one is given, `stream` its current stream."""
     if stream is not None:
+        _same_device(what, dev, stream)
         return torch.cuda.stream(stream)
     if dev >= 0 and dev != torch.cuda.current_device():
         return torch.cuda.device(dev)
@@ -324,6 +330,8 @@ def _call(fn, dev: int, stream, args) -> int:
     """fn(*args, stream) with device `dev` current; the stream is its current one unless given."""
     if dev < 0:
         raise DeamoeError(ERR_INVALID, f"{fn.__name__}: tensors are not on a GPU")
+    if stream is not None:
+        _same_device(fn.__name__, dev, stream)
     if dev != torch.cuda.current_device():
         with torch.cuda.device(dev):
             return _call(fn, dev, stream, args)
@@ -339,7 +347,7 @@ def _run_with_workspace(fn, dev: int, stream, ws, nbytes: int, *args):
     """The same for a call whose last two arguments are its workspace: the given one, or one of torch's
     for the stream that the call runs on."""
     if ws is None and nbytes and dev >= 0:
-        with contextlib.nullcontext() if stream is None else _on(dev, stream):
+        with contextlib.nullcontext() if stream is None else _on(fn.__name__, dev, stream):
             ws = torch.empty(nbytes, dtype=torch.uint8, device=torch.device("cuda", dev))
     elif ws is not None and (ws.get_device() != dev or not ws.is_contiguous()):
         raise DeamoeError(ERR_WORKSPACE, f"{fn.__name__}: workspace is not contiguous, or not on device {dev}")
@@ -546,7 +554,7 @@ class W4Experts:
     def __call__(self, x, topk_ids, topk_w, y=None, stream=None):
         """y [T, h] from x [T, h] (bf16), topk_ids [T, k] (int32, -1: none) and topk_w [T, k] (fp32)."""
         if stream is not None:
-            with _on(x.get_device(), stream):
+            with _on("W4Experts", x.get_device(), stream):
                 return self(x, topk_ids, topk_w, y)
         T, k = topk_ids.shape
         new, i32 = dict(device=x.device), torch.int32
@@ -574,7 +582,7 @@ class Block:
         """z, or with w_next (z, u): u is the next block's normed input, which its call takes in
         place of norming x again.  Further keyword arguments go to the layer, which runs with x's
         device and the call's stream as the current ones."""
-        with _on(x.get_device(), stream):
+        with _on("Block", x.get_device(), stream):
             if u is None:
                 u = torch.empty_like(x)
                 deamoe_prenorm(x, self.w_pre, u, eps=self.eps)

@@ -1,4 +1,5 @@
-"""The binding of the operators beside the layer, on the CPU: which device and stream a call runs on."""
+"""The binding of the operators beside the layer, on the CPU: which device and stream a call runs on,
+and what is refused before the library is called."""
 import contextlib
 import os
 import sys
@@ -48,6 +49,12 @@ def gpus(monkeypatch):
     return lambda: (state["device"], state[state["device"]])
 
 
+def refused(f, *a, status=D.ERR_INVALID, **kw):
+    with pytest.raises(D.DeamoeError) as e:
+        f(*a, **kw)
+    assert e.value.status == status, str(e.value)
+
+
 @pytest.mark.parametrize("stream", [None, Stream(1, "side")])
 def test_a_blocks_layer_runs_where_its_rows_are(gpus, monkeypatch, stream):
     """Norms and layer run on the same device and stream, that of x and the call, also where another
@@ -73,3 +80,16 @@ def test_a_call_runs_on_its_tensors_device(gpus):
     assert D._call(fn, 1, None, (7,)) == ((7, "default 1"), (1, "default 1"))
     assert D._call(fn, 1, Stream(1, "side"), (7,))[0] == (7, "side")
     assert D._call(fn, 0, None, (7,)) == ((7, "default 0"), (0, "default 0"))
+
+
+def test_a_stream_of_another_device_is_refused(gpus):
+    def fn(*args):
+        raise AssertionError("called")
+
+    far = Stream(0, "far")
+    refused(D._call, fn, 1, far, ())
+    refused(D._run_with_workspace, fn, 1, far, None, 64)
+    x, w = (torch.zeros(*s).as_subclass(OnSecond) for s in ((4, 8), (8,)))
+    refused(D.Block(fn, w, w), x, stream=far)
+    pair = (torch.zeros(2, 4, 4, dtype=torch.uint8), torch.zeros(2, 4, 1))
+    refused(D.W4Experts(pair, pair, pair), x, torch.zeros(4, 1, dtype=torch.int32), torch.zeros(4, 1), stream=far)
