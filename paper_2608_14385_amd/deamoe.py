@@ -377,6 +377,8 @@ def deamoe_dispatch(ids, x, offset, pair, row, xs=None, ws=None, stream=None):
     with xs [T * k, h] the rows of x [T, h] in that order (x may be None without xs)."""
     what, i32 = "deamoe_dispatch", torch.int32
     T, k = _rows(what, ids, "ids")
+    if offset is None:
+        raise DeamoeError(ERR_INVALID, f"{what}: offset is needed")
     dev, n, h, act = ids.get_device(), offset.numel() - 1, 1, F32
     _fits(what, dev, ("ids", ids, i32, (T, k)), ("offset", offset, i32, (n + 1,)),
           ("pair", pair, i32, (T * k,)), ("row", row, i32, (T, k)))
@@ -431,6 +433,8 @@ def _w4(what: str, x, matrices, y, offset):
     """Checks one product's tensors: its config, rows and device."""
     codes, scale = matrices[0]
     M, K = _rows(what, x, "x")
+    if codes is None or scale is None:
+        raise DeamoeError(ERR_INVALID, f"{what}: codes and scale are needed")
     shape, groups = codes.shape, scale.shape[-1] if scale.dim() else 0
     if len(shape) not in (2, 3) or shape[-1] * 2 != K or scale.dim() != len(shape) or not groups or K % groups:
         raise DeamoeError(ERR_INVALID, f"{what}: codes {tuple(shape)} and scale {tuple(scale.shape)} "

@@ -93,3 +93,20 @@ def test_a_stream_of_another_device_is_refused(gpus):
     refused(D.Block(fn, w, w), x, stream=far)
     pair = (torch.zeros(2, 4, 4, dtype=torch.uint8), torch.zeros(2, 4, 1))
     refused(D.W4Experts(pair, pair, pair), x, torch.zeros(4, 1, dtype=torch.int32), torch.zeros(4, 1), stream=far)
+
+
+def test_every_missing_tensor_is_refused():
+    i32, bf = torch.int32, torch.bfloat16
+    ids, x, xs = torch.zeros(4, 2, dtype=i32), torch.zeros(4, 8, dtype=bf), torch.zeros(8, 8, dtype=bf)
+    off, pair, w, v = torch.zeros(9, dtype=i32), torch.zeros(8, dtype=i32), torch.zeros(4, 2), torch.zeros(8, dtype=bf)
+    codes, scale = torch.zeros(5, 64, dtype=torch.uint8), torch.zeros(5, 1)
+    rows, out = torch.zeros(6, 128, dtype=bf), torch.zeros(6, 5, dtype=bf)
+    for f, args in ((D.deamoe_dispatch, (ids, x, off, pair, ids, xs)), (D.deamoe_dispatch_backward, (ids, xs, x)),
+                    (D.deamoe_combine, (ids, w, xs, x)), (D.deamoe_w4_linear, (rows, codes, scale, out)),
+                    (D.deamoe_w4_swiglu, (rows, codes, scale, codes, scale, out)),
+                    (D.deamoe_prenorm, (x, v, x)), (D.deamoe_prenorm_backward, (x, v, x, x, v.float())),
+                    (D.deamoe_postnorm, (x, x, v, x)), (D.deamoe_postnorm_backward, (x, v, x, x, x, v.float()))):
+        for i in range(len(args)):
+            if f is D.deamoe_dispatch and i == 5:   # the lists alone
+                continue
+            refused(f, *args[:i], None, *args[i + 1:])
