@@ -354,7 +354,16 @@ def _run_with_workspace(fn, dev: int, stream, ws, nbytes: int, *args):
     _run(fn, dev, stream, *args, _ptr(ws), 0 if ws is None else ws.numel() * ws.element_size())
 
 
+_INT32 = (1 << 31) - 1   # ctypes passes larger sizes on modulo 2^32
+
+
+def _too_large(what: str, name: str, sizes):
+    raise DeamoeError(ERR_UNSUPPORTED, f"{what}: {name} {tuple(sizes)} has sizes past 2^31 - 1")
+
+
 def _bytes(fn, *args) -> int:
+    if max(args) > _INT32:
+        _too_large(fn.__name__, "sizes", args)
     n = C.c_size_t(0)
     _check(fn(*args, C.byref(n)), fn.__name__)
     return n.value
@@ -364,7 +373,10 @@ def _rows(what: str, t: torch.Tensor, name: str) -> tuple:
     if t is None or t.dim() != 2:
         raise DeamoeError(ERR_INVALID, f"{what}: {name} is "
                           f"{'missing' if t is None else tuple(t.shape)}, needed are two dimensions")
-    return t.shape
+    shape = t.shape
+    if shape[0] > _INT32 or shape[1] > _INT32:
+        _too_large(what, name, shape)
+    return shape
 
 
 @functools.lru_cache(maxsize=1024)   # of sizes alone; 10 pairs sorted in 8.5 us, not 8.9
@@ -380,6 +392,8 @@ def deamoe_dispatch(ids, x, offset, pair, row, xs=None, ws=None, stream=None):
     if offset is None:
         raise DeamoeError(ERR_INVALID, f"{what}: offset is needed")
     dev, n, h, act = ids.get_device(), offset.numel() - 1, 1, F32
+    if n > _INT32:
+        _too_large(what, "offset", offset.shape)
     _fits(what, dev, ("ids", ids, i32, (T, k)), ("offset", offset, i32, (n + 1,)),
           ("pair", pair, i32, (T * k,)), ("row", row, i32, (T, k)))
     if xs is not None:
@@ -440,6 +454,8 @@ def _w4(what: str, x, matrices, y, offset):
         raise DeamoeError(ERR_INVALID, f"{what}: codes {tuple(shape)} and scale {tuple(scale.shape)} "
                                        f"do not fit {K} columns")
     n, R, dev, sdt, bf16 = shape[0] if len(shape) == 3 else 1, shape[-2], x.get_device(), scale.dtype, torch.bfloat16
+    if n > _INT32 or R > _INT32:
+        _too_large(what, "codes", shape)
     if sdt is not torch.float32 and sdt is not bf16:
         raise DeamoeError(ERR_INVALID, f"{what}: scale is {sdt}")
     for c, s in matrices:

@@ -110,3 +110,32 @@ def test_every_missing_tensor_is_refused():
             if f is D.deamoe_dispatch and i == 5:   # the lists alone
                 continue
             refused(f, *args[:i], None, *args[i + 1:])
+
+
+def test_sizes_past_32_bits_are_refused():
+    """2^32 + 4 would reach the library as 4, which it would answer."""
+    far, bf, un = (1 << 32) + 4, torch.bfloat16, D.ERR_UNSUPPORTED
+
+    def meta(*shape, dtype=bf):
+        return torch.empty(*shape, dtype=dtype, device="meta")
+
+    for T, h in ((far, 8), (2, far)):
+        x, v, f = meta(T, h), meta(h), meta(h, dtype=torch.float32)
+        refused(D.deamoe_prenorm, x, v, x, status=un)
+        refused(D.deamoe_prenorm_backward, x, v, x, x, f, status=un)
+        refused(D.deamoe_postnorm, x, x, v, x, status=un)
+        refused(D.deamoe_postnorm_backward, x, v, x, x, x, f, status=un)
+        row, w = meta(T, 1, dtype=torch.int32), meta(T, 1, dtype=torch.float32)
+        refused(D.deamoe_combine, row, w, x, x, status=un)
+        refused(D.deamoe_combine_backward, row, w, x, x, x, w, status=un)
+        refused(D.deamoe_dispatch_backward, row, x, x, status=un)
+        refused(D.deamoe_dispatch, row, x, meta(5, dtype=torch.int32), meta(T, dtype=torch.int32), row, x, status=un)
+    for M, n, R, K in ((far, 1, 8, 64), (2, 1, far, 64), (2, 1, 8, far - 4 + 64), (2, far, 8, 64)):
+        codes, scale = meta(n, R, K // 2, dtype=torch.uint8), meta(n, R, K // 64)
+        x, y, off = meta(M, K), meta(M, R), meta(n + 1, dtype=torch.int32)
+        refused(D.deamoe_w4_linear, x, codes, scale, y, offset=off, status=un)
+        refused(D.deamoe_w4_swiglu, x, codes, scale, codes, scale, y, offset=off, status=un)
+    ids = meta(4, 2, dtype=torch.int32)
+    refused(D.deamoe_dispatch, ids, None, meta(far + 1, dtype=torch.int32), meta(8, dtype=torch.int32), ids, status=un)
+    refused(D.deamoe_dispatch_workspace_bytes, far, 2, 8, status=un)
+    refused(D.deamoe_norm_workspace_bytes, far, 8, status=un)
