@@ -141,6 +141,13 @@ struct W4Args {
   const void *w[2], *scale[2];   // gate and up, or one matrix
   void *y;
 };
+// Workgroups of the streaming kernel that a CU holds at once.  A workgroup is a
+// wave on each of the four SIMDs: three fit up to 168 registers and 53 KB of LDS.
+// Two matrices in groups of 32 take 169, four weight tiles (nr) per wave about 256,
+// two token tiles (ntt) 209 to 233 and 73 KB; a wide panel takes the LDS for itself.
+constexpr int stream_resident(int mats, int nr, int ntt, int group, bool wide) {
+  return wide ? 1 : nr > 1 || ntt > 1 || (mats == 2 && group == 32) ? 2 : 3;
+}
 hipError_t launch_w4(const W4Args &a, int mats, hipStream_t s);
 
 // ---- norm.hip

@@ -616,12 +616,13 @@ int64_t row_tiles(const W4Args &a, int rows) {
 dim3 grid_of(int64_t items) { return dim3((unsigned)(items < (1 << 20) ? items : 1 << 20)); }
 
 // K parts of the streaming kernel's workgroups, which there are `groups` of with
-// one part: as many as keep all workgroups on the CUs at once, of which each
-// holds three (two token tiles: two), and as a panel holds a round of the ring
-// for.  us, one | two | four parts: 4096 x 7168, one row, 64 workgroups of one
+// one part: as many as keep all workgroups on the CUs at once (stream_resident
+// each), and as a panel holds a round of the ring for.  us, one | two | four parts: 4096 x 7168, one row, 64 workgroups of one
 // part, 20.5 | 13.5 | 9.7; 16384 x 7168, 256 of them, 22.0 | 16.9 | 21.8; 28672 x
 // 7168, 448 of them, 26.8 | 31.3 | 33.1; 8 rows of 8 experts of 2 x 2048 x 7168,
-// 256 of them, 31.8 | 27.7 | 34.9.
+// 256 of them, 31.8 | 27.7 | 34.9.  Groups of 32, two matrices, of which a CU holds
+// two workgroups: 257 of them, 16448 x 2048 of one row, 18.8 | 22.8; 384, 24576 x
+// 4096 of 16 rows, 38.3 | 51.4; 320, one row of 10 experts of 2048 x 4096, 34.7 | 43.0.
 struct Parts {
   int ks, columns;   // K parts, columns of a panel
 };
@@ -649,7 +650,8 @@ hipError_t stream(const W4Args &a, hipStream_t s) {
   constexpr int kCus = 256;
   const int64_t tiles = row_tiles(a, kTile * NTT);
   const int64_t groups = tiles * ((a.R + kWaves * NR * kTile - 1) / (kWaves * NR * kTile));
-  const Parts p = k_parts(a, NTT, groups, kCus * (NTT == 1 ? 3 : 2), panel_words(NTT, false), kPanelScales);
+  const int most = kCus * stream_resident(MATS, NR, NTT, a.group, false);
+  const Parts p = k_parts(a, NTT, groups, most, panel_words(NTT, false), kPanelScales);
   if constexpr (NR == 1 && NTT == 1) {
     // With no more workgroups than CUs, panels that fill a CU's LDS, where they
     // allow more parts or are four times as wide; us, narrow | wide: 4096 x 7168,
