@@ -691,7 +691,11 @@ hipError_t run(const W4Args &a, hipStream_t s) {
     if (MATS == 1 && row_tiles(a, kTile) * ((a.R + 63) / 64) >= 5120) return stream<1, 4, 1, false>(a, s);
     return stream<MATS, 1, 1, false>(a, s);
   }
-  if ((int64_t)((a.M + 63) / 64) * blocks >= 256) return tile<MATS>(a, s);
+  // The tiled kernel from more than one workgroup on every second CU on, us, streamed |
+  // tiled: 4096 x 4096, 59 | 60 at 448 rows (112 workgroups), 74 | 61 at 640 (160);
+  // 7168 x 7168, 82 | 99 at 192 (84), 126 | 100 at 320 (140), 166 | 102 at 512 (224);
+  // two matrices of 4096 x 4096, 43 | 59 at 192 (96), 79 | 60 at 384 (192).
+  if ((int64_t)((a.M + 63) / 64) * blocks > 128) return tile<MATS>(a, s);
   if (a.M <= kTile) return stream<MATS, 1, 1, false>(a, s);
   // two token tiles per pass over the weights, us, one | two: 4096 x 4096, 22.8 |
   // 25.8 at 128 rows, 38.9 | 34.4 at 256; two matrices 53 | 64 at 200

@@ -63,3 +63,9 @@ def test_experts(rows, R, K, group, scale):
         at = slice(int(offset[e]), int(offset[e + 1]))
         want = wanted(x[at], [(c[e], s[e]) for c, s in mats], group)
         assert torch.equal(y[at], want[0]) and torch.equal(z[at], want[1]), e
+
+
+@pytest.mark.parametrize("M,R,K,group", [(384, 5000, 192, 64), (385, 5000, 192, 64),     # 120 and 140 workgroups
+                                         (64, 16000, 160, 32), (65, 16000, 160, 32)])    # two matrices: 126 and 252
+def test_either_side_of_the_tiled_kernel(M, R, K, group):
+    test_one_matrix(M, R, K, group, F32)
