@@ -682,10 +682,13 @@ hipError_t run(const W4Args &a, hipStream_t s) {
   const int blocks = (a.R + 255) / 256 * MATS;
   if (a.offset) {
     // The mean rows of a matrix decide, us, streamed | tiled: 64 experts of 2 x
-    // 1280 x 2048, 54 | 98 at 12 rows, 88 | 99 at 24, 124 | 106 at 36; of 2048 x
-    // 1280, 44 | 43 at 12 rows, 65 | 56 at 24.
+    // 1280 x 2048, 57 | 78 at 12 rows, 77 | 79 at 19, 96 | 83 at 24; 128 of 2 x 1536 x
+    // 4096, 304 | 309 at 20, 353 | 309 at 24; 256 of 2 x 512 x 2048, 121 | 127 at 20,
+    // 141 | 129 at 24.  One matrix: 64 of 2048 x 1280, 36 | 37 at 7, 49 | 49 at 15, 59 |
+    // 49 at 19; 128 of 4096 x 1536, 161 | 170 at 14, 201 | 172 at 20; 16 of 7168 x 2048,
+    // 52 | 52 at 14.
     const int64_t mean = a.M / a.n;
-    if (mean > (MATS == 2 ? 28 : 14)) return tile<MATS>(a, s);
+    if (mean > (MATS == 2 ? 20 : 14)) return tile<MATS>(a, s);
     // Many workgroups, of one matrix: four weight tiles per wave (82 experts of
     // 4096 x 1536: 81 -> 75 us; but 48 of 2048 x 1280 34 -> 41).
     if (MATS == 1 && row_tiles(a, kTile) * ((a.R + 63) / 64) >= 5120) return stream<1, 4, 1, false>(a, s);

@@ -69,3 +69,9 @@ def test_experts(rows, R, K, group, scale):
                                          (64, 16000, 160, 32), (65, 16000, 160, 32)])    # two matrices: 126 and 252
 def test_either_side_of_the_tiled_kernel(M, R, K, group):
     test_one_matrix(M, R, K, group, F32)
+
+
+@pytest.mark.parametrize("each", [14, 15, 20, 21])   # the last streamed and the first tiled, one matrix and two
+def test_either_side_of_the_tiled_kernel_for_experts(each):
+    test_experts((each,) * 9, 150, 1120, 32, F32)
+    test_experts((1, 2 * each, 0, 2 * each, each - 1), 150, 1120, 32, F32)   # the same mean, unevenly
