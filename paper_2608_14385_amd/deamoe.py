@@ -370,13 +370,14 @@ def _bytes(fn, *args) -> int:
 
 
 def _rows(what: str, t: torch.Tensor, name: str) -> tuple:
-    if t is None or t.dim() != 2:
-        raise DeamoeError(ERR_INVALID, f"{what}: {name} is "
-                          f"{'missing' if t is None else tuple(t.shape)}, needed are two dimensions")
-    shape = t.shape
-    if shape[0] > _INT32 or shape[1] > _INT32:
-        _too_large(what, name, shape)
-    return shape
+    try:
+        rows, cols = t.shape
+    except (AttributeError, ValueError):
+        raise DeamoeError(ERR_INVALID, f"{what}: {name} is {'missing' if t is None else tuple(t.shape)}, "
+                                       "needed are two dimensions") from None
+    if rows > _INT32 or cols > _INT32:
+        _too_large(what, name, (rows, cols))
+    return rows, cols
 
 
 @functools.lru_cache(maxsize=1024)   # of sizes alone; 10 pairs sorted in 8.5 us, not 8.9
@@ -389,11 +390,11 @@ def deamoe_dispatch(ids, x, offset, pair, row, xs=None, ws=None, stream=None):
     with xs [T * k, h] the rows of x [T, h] in that order (x may be None without xs)."""
     what, i32 = "deamoe_dispatch", torch.int32
     T, k = _rows(what, ids, "ids")
-    if offset is None:
-        raise DeamoeError(ERR_INVALID, f"{what}: offset is needed")
-    dev, n, h, act = ids.get_device(), offset.numel() - 1, 1, F32
-    if n > _INT32:
-        _too_large(what, "offset", offset.shape)
+    try:
+        n = offset.numel() - 1   # past 32 bits: the workspace's size refuses it
+    except AttributeError:
+        raise DeamoeError(ERR_INVALID, f"{what}: offset is needed") from None
+    dev, h, act = ids.get_device(), 1, F32
     _fits(what, dev, ("ids", ids, i32, (T, k)), ("offset", offset, i32, (n + 1,)),
           ("pair", pair, i32, (T * k,)), ("row", row, i32, (T, k)))
     if xs is not None:
