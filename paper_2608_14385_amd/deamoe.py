@@ -289,7 +289,9 @@ class Layer:
 # Operators beside the layer: sorted tokens, 4-bit products, norms.  Tensors
 # are contiguous and on one device, outputs are the caller's; the calls run on
 # `stream` (default: the current stream of the tensors' device) and, where no
-# workspace is given, take one from torch's allocator for that stream.
+# workspace is given, take one from torch's allocator for that stream.  None of
+# them, nor the classes below, is recorded by autograd: results carry no gradient
+# history, also of inputs that require one; gradients are the _backward calls.
 
 
 def _fits(what: str, dev: int, *tensors):
@@ -565,7 +567,12 @@ class W4Experts:
     experts' products over their rows, and the weighted way back.
 
     gate, up and down are (codes, scale) pairs: gate and up [n, d, h / 2] and [n, d, h / group], down
-    [n, h, d / 2] and [n, h, d / group]."""
+    [n, h, d / 2] and [n, h, d / group].
+
+    Forward only: 4-bit products have no gradient here, and the result is detached from its inputs.
+    The activations and every expert's row of the down product are rounded to bf16, the products'
+    output type, before the weighted sum in fp32 (Layer keeps those rows in fp32): rows of half the
+    bytes for the way back, at half a bf16 step, 2^-8, of each row's share of y."""
 
     def __init__(self, gate, up, down):
         self.gate, self.up, self.down = gate, up, down
@@ -592,7 +599,8 @@ class W4Experts:
 
 class Block:
     """A layer between its norms: z = res_scale * x + gate * RMSNorm(layer(RMSNorm(x) * w_pre)) * w_post,
-    the layer being a Layer or any callable of the normed rows."""
+    the layer being a Layer or any callable of the normed rows.  Forward only: z is detached from x and
+    the weights (deamoe_postnorm_backward and deamoe_prenorm_backward give the norms' gradients)."""
 
     def __init__(self, layer, w_pre, w_post, gate=None, res_scale: float = 1.0, eps: float = 1e-6,
                  w_next=None):
