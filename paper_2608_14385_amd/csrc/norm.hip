@@ -179,8 +179,17 @@ __global__ __launch_bounds__(MAXG) void postnorm_kernel(PostnormArgs a) {
 // the one after it with the next one before.  A workgroup walks over rows t,
 // t + grid, ... and keeps its sums over them for its columns: in registers, or
 // for wide rows in its part of the workspace.  Rows that one wave holds are taken
-// four at a time, a wave each (blockDim.y), whose sums are joined in LDS.  8192 rows of 4096 in bf16 with both
-// norms and a shared gate, 403 MB, take 89 us: 4.5 TB/s, of a copy's 4.9.
+// four at a time, a wave each (blockDim.y), whose sums are joined in LDS.  8192 rows
+// of 4096 in bf16 with both norms and a shared gate, 403 MB, take 89 us: 4.5 TB/s, of
+// a copy's 4.9.
+//   Two chunks in each of 1024 threads (fp32 rows of 4097 to 8192 columns, bf16 of
+// 8193 to 16384) leave 128 registers, and four of those six forms keep a part of
+// the row, its successor or the sums in scratch: fp32 with both norms 61 registers,
+// bf16 30 (pre), 70 (post) and 174 (both).  2048 rows with both norms: fp32 of 5120
+// 113 us, of 7168 128 (floors 51 and 71; 471 MB read for 235, 187 written for 117);
+// bf16 of 9216 302 us, of 12288 312, of 16384 335 (floors 46, 61 and 82; 1130 MB read
+// for 201 and 604 written for 101 at 12288).  The two forms that do not spill are
+// within 1.4 of their floors.
 enum NormMode : int { NORM_PRE = 0, NORM_POST = 1, NORM_BOTH = 2 };
 
 template <bool F32, int N, int MODE>
@@ -388,7 +397,8 @@ namespace {
 // hold it with two chunks each while that leaves several rows per CU; from 4097
 // bf16 columns on one chunk each, in 1024 threads (the gradient of 2048 rows of
 // 7168: 71 us with 512 threads of two chunks, 50 with these); rows wider than
-// 2048 chunks are not held.
+// 2048 chunks are not held (the same of 2048 rows of 16400: 344 us, held ones of
+// 16384 335; in fp32 of 8200 and 8192 columns 197 and 134).
 struct Shape {
   int threads, held;
 };

@@ -188,10 +188,11 @@ __device__ inline void rows_together(u32x4 &a, u32x4 &b) {
 }  // namespace
 
 // Few token rows: the weights are streamed, each byte once per 16 * NTT rows
-// (KEEP: through the caches, for another 16 rows to come).  A wave takes NR
-// 16-row tiles of each matrix and every ks-th step of 256 columns.  The loads of
-// a step are requested two steps ahead, straight into
-// registers, each load 8 whole cache lines (halves of 16 lines streamed at 4.8
+// (KEEP, dense products of more than 16 rows: through the caches, for another 16
+// to come; experts' products never, though the few experts of more than 16 rows
+// then read their codes again).  A wave takes NR 16-row tiles of each matrix and
+// every ks-th step of 256 columns.  The loads of a step are requested two steps
+// ahead, straight into registers, each load 8 whole cache lines (halves of 16 lines streamed at 4.8
 // TB/s, these at 5.6, by loads alone on 490 MB).  The token rows
 // stand in LDS, a panel of columns at a time, already in the codes' order: read
 // from memory by every wave they would take several times the weights'
@@ -201,9 +202,14 @@ __device__ inline void rows_together(u32x4 &a, u32x4 &b) {
 // lines as the weights.  Waves that share tiles add their sums over LDS at the
 // end.  Every panel costs a round trip to the caches, so that WIDE panels take
 // all of a CU's LDS where a CU has one workgroup.
-// 82 of 128 experts of 2 x 1536 x 4096 for 16 tokens, 490 MB, take 90 us: 5.5 TB/s,
-// bound by HBM.  7168 x 7168 for one row takes 11 us, of which the weights'
-// 27 MB need 5.5.
+// About 75 of 128 experts of 2 x 1536 x 4096 for 16 tokens, 490 MB, take 90 to 93 us:
+// 5.3 to 5.5 TB/s, bound by HBM, which reads 1.02 times the touched weights.  About
+// 75 experts of 4096 x 1536, 246 MB, take 73 us, 3.4 TB/s: a workgroup finds its item
+// in two dependent round trips, for six steps of work.  7168 x 7168 for one row takes
+// 11 us, of which the weights' 27 MB need 5.5.  Dense products of 8 rows and more
+// are far from their weights' time: every 16 token rows read and unpack all codes
+// again, and every workgroup all of K (4096 x 4096: 9.8 us at 8 rows, 17 at 64, 22 at
+// 128, 31 at 256).
 constexpr int kPanelWords = 16 * (1024 + 8) / 2;   // of a token tile, 4 bytes each
 constexpr int kPanelScales = 32;                   // of a weight row, at most
 constexpr int kWidePanel = 4;                      // token tiles' words in a wide panel
@@ -425,12 +431,14 @@ __global__ __launch_bounds__(kThreads, 2) void w4_stream_kernel(W4Args a, int ks
 // Both operands of the next step are requested before a step's products; the
 // token rows go through registers, where they take the codes' order, into the
 // other half of the LDS buffer.
-// 8192 rows through 2048 x 8192 run at 840 TFLOP/s; 12288 rows through 64 experts
-// of 2 x 1280 x 2048, whose tiles are a seventh empty and whose sums are short, in
-// 209 us, 616 TFLOP/s.  A step's 32 KB for 4 MFLOP keep a CU's loads at 19 bytes
-// per ns, near the 21 of a stream from HBM on all CUs, and unpacking takes about
-// half as many issue cycles as the products; more steps in flight, wider
-// workgroups and pairs of steps were no faster.
+// 8192 rows through 2048 x 8192 run at 810 to 840 TFLOP/s; 12288 rows through 64
+// experts of 2 x 1280 x 2048, whose tiles are a seventh empty and whose sums are
+// short, in 210 us, 610 TFLOP/s.  There the matrix cores are busy for 29 % of the
+// time, HBM reads 1.4 TB/s and four of five requests hit L2, so that none of them
+// is the bound: a step's 32 KB per workgroup arrive at 19 bytes per ns on a CU with
+// one step on its way, and by instruction count unpacking takes half as many issue
+// cycles as the products.  Weights requested two steps at a time spilled registers,
+// 215 -> 224 us.
 constexpr int kTileTok = 64, kTileStep = 128, kTileStride = kTileStep + 8;
 constexpr int kTileThreads = 256, kTileWaves = kTileThreads / kWave, kTileWeights = 4;
 template <int MATS, int G32>
@@ -689,7 +697,7 @@ hipError_t run(const W4Args &a, hipStream_t s) {
     // 52 | 52 at 14.
     const int64_t mean = a.M / a.n;
     if (mean > (MATS == 2 ? 20 : 14)) return tile<MATS>(a, s);
-    // Many workgroups, of one matrix: four weight tiles per wave (82 experts of
+    // Many workgroups, of one matrix: four weight tiles per wave (about 75 experts of
     // 4096 x 1536: 81 -> 75 us; but 48 of 2048 x 1280 34 -> 41).
     if (MATS == 1 && row_tiles(a, kTile) * ((a.R + 63) / 64) >= 5120) return stream<1, 4, 1, false>(a, s);
     return stream<MATS, 1, 1, false>(a, s);
